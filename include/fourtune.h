@@ -332,6 +332,122 @@ ft_status ft_linear_bwd_input_nvfp4(const uint8_t *gq, const uint8_t *gs, const 
                                     const uint8_t *wq, const uint8_t *ws, const float *wt, int64_t K,
                                     float *dx, hipStream_t stream);
 
+/*
+ * ---- 8-bit activations and gradients over the same frozen weight ----
+ *
+ * MXFP8: E4M3 codes (OCP: bias 7, largest 448, no infinities), one per byte,
+ * with one E8M0 scale per 32 consecutive elements of a row.  Block rule: the
+ * smallest e >= -127 with max|v| <= 448 * 2^e (nothing saturates; a zero block
+ * gets e = -127), scale byte = e + 127, each element the nearest E4M3 value of
+ * v / 2^e, ties to the even code.  A block that holds an infinity or NaN gets
+ * scale byte 255 (the E8M0 NaN), which makes it NaN in every product.
+ * Layout: codes [rows, cols]; scales [ceil(cols / 128), rows, 4], block 4 g + j
+ * of row m at [g, m, j]; places past the row's last block hold 127 (a scale of
+ * 1) when written here and are ignored when read.  Four blocks of a row are
+ * thus one dword, and the rows of a GEMM tile one run of memory.
+ *
+ * The weight is ft_quantize_blockwise's (block_rows = 32), and so are D, U and
+ * the adapter gradients: ft_lora_grads takes these calls' P, Qp and bf16
+ * tensors unchanged.
+ */
+typedef enum ft_act { FT_ACT_NONE = 0, FT_ACT_GELU = 1, FT_ACT_SILU = 2, FT_ACT_RELU = 3 } ft_act;
+
+/*
+ * RMS norm of the residual stream, with the stream's addition in front and an
+ * MXFP8 output behind:
+ *   h[m,k] = bf16(x[m,k] + residual[m,k])             (h = x without a residual)
+ *   rstd[m] = 1 / sqrt(mean_k h[m,k]^2 + eps)
+ *   y[m,k] = h[m,k] rstd[m] w[k]
+ *   codes, scales = MXFP8(y), from y in fp32;  y is stored in bf16
+ *   x, residual  bf16 [rows, cols]; residual may be NULL.
+ *   w            bf16 [cols].
+ *   h            bf16 [rows, cols]; required with a residual, NULL without one.
+ *                It may be x or residual itself (the stream updated in place).
+ *   y            bf16 [rows, cols] or NULL (input of the low-rank branch, of
+ *                the adapter gradients, or of a bf16 layer).
+ *   codes, scales  MXFP8 of y, or both NULL.  y or codes is required.
+ *   rstd         fp32 [rows] or NULL (kept for ft_rmsnorm_bwd).
+ * cols % 32 == 0, cols <= 16384 (FT_ERR_UNSUPPORTED above); eps >= 0.
+ * rows == 0 is a no-op.
+ */
+ft_status ft_rmsnorm_quantize8(const void *x, const void *residual, const void *w, int64_t rows, int64_t cols,
+                               float eps, void *h, void *y, uint8_t *codes, uint8_t *scales, float *rstd,
+                               hipStream_t stream);
+
+/*
+ * Gradients of the norm: with g = dy * w and n = h * rstd,
+ *   dx[m,k] = dh[m,k] + rstd[m] (g[m,k] - n[m,k] mean_k(g n))
+ *   dw[k]   = sum_m dy[m,k] n[m,k]
+ * dx is the gradient of x and of residual alike.
+ *   dy, h, w, rstd  as in the forward; rstd as it wrote it.
+ *   dh           bf16 [rows, cols] or NULL: the gradient that reaches h on the
+ *                residual stream.
+ *   dx           bf16 [rows, cols]; it may be dy or dh itself.
+ *   dw           fp32 [cols], or NULL (a frozen w).
+ *   workspace    ft_rmsnorm_bwd_workspace_size(rows, cols) bytes, 16-byte
+ *                aligned, where dw is wanted: fp32 partial sums over runs of
+ *                rows, added in a fixed order.  Calls that share one must not
+ *                overlap.
+ * rows == 0 gives dw = 0.
+ */
+ft_status ft_rmsnorm_bwd(const void *dy, const void *dh, const void *h, const void *w, const float *rstd, int64_t rows,
+                         int64_t cols, void *dx, float *dw, void *workspace, size_t workspace_bytes,
+                         hipStream_t stream);
+size_t ft_rmsnorm_bwd_workspace_size(int64_t rows, int64_t cols);
+
+/*
+ * MXFP8 quantization of a bf16 matrix, optionally fused with the low-rank
+ * down-projection of the same rows, or of a gradient on its way back through an
+ * activation.
+ *   src          bf16 [rows, cols]; cols % 32 == 0.
+ *   z, act, v    z bf16 [rows, cols] (ft_linear8_fwd's): what is quantized is
+ *                src * act'(z), in fp32, which v (bf16 [rows, cols], or NULL)
+ *                receives too; v may be src.  act is not FT_ACT_NONE then.
+ *                z NULL: src itself; act is FT_ACT_NONE and v NULL.
+ *   codes, scales  MXFP8, layout as above.
+ *   proj, R, proj_layout, proj_out, workspace  as in ft_quantize_blockwise, for
+ *                src itself (FT_ERR_UNSUPPORTED together with z: quantize v).
+ * rows == 0 is a no-op.  cols <= 2^20.
+ */
+ft_status ft_quantize8(const void *src, const void *z, ft_act act, int64_t rows, int64_t cols, void *v, uint8_t *codes,
+                       uint8_t *scales, const void *proj, int32_t R, ft_proj_layout proj_layout, float *proj_out,
+                       void *workspace, size_t workspace_bytes, hipStream_t stream);
+size_t ft_quantize8_workspace_size(int64_t rows, int64_t cols, int32_t R, ft_proj_layout proj_layout);
+
+/*
+ * Forward of the triple-branch linear on 8-bit activations:
+ *   a[m,n] = sum_k DQ(xq)[m,k] DQ(wq)[n,k] + sum_j P[m,j] U[j,n] + bias[n]
+ *   z[m,n] = bf16(a[m,n]);   y[m,n] = act(a[m,n]) + residual[m,n]
+ * FP8 x FP4 block-scaled MFMA, fp32 throughout, one rounding of each output.
+ *   xq, xs   X in MXFP8 [M, K], scales [ceil(K / 128), M, 4].
+ *   wq, ws, P, R, U, bias  as in ft_linear_fwd.
+ *   act      FT_ACT_NONE; FT_ACT_GELU (the tanh form); FT_ACT_SILU,
+ *            a / (1 + exp(-a)); FT_ACT_RELU.
+ *   residual [M, N] of y's type, or NULL; it may be y itself.
+ *   z        bf16 [M, N] or NULL: saved for ft_quantize8 or ft_linear8_bwd_input.
+ *   y        [M, N], bf16 or fp32.
+ * FT_ERR_UNSUPPORTED: K > 65536, N > 2^20, N K / 2, or M K / 32 from 2 GiB on.
+ */
+ft_status ft_linear8_fwd(const uint8_t *xq, const uint8_t *xs, int64_t M, int64_t K, const uint8_t *wq,
+                         const uint8_t *ws, int64_t N, const float *P, int32_t R, const void *U, const void *bias,
+                         ft_act act, const void *residual, void *z, void *y, ft_dtype y_dtype, hipStream_t stream);
+
+/*
+ * Input gradient of the same layer on 8-bit gradients, optionally through the
+ * activation of the layer in front (whose z it takes) and added to a gradient
+ * that reaches the same tensor another way:
+ *   dx[m,k] = (sum_n DQ(gq)[m,n] DQ(wq)[n,k] + sum_j Qp[m,j] D[k,j]) act'(z[m,k]) + residual[m,k]
+ *   gq, gs   G in MXFP8 [M, N], scales [ceil(N / 128), M, 4].
+ *   wq, ws, Qp, R, D  as in ft_linear_bwd_input.
+ *   z, act   bf16 [M, K] and its activation, or NULL and FT_ACT_NONE.
+ *   residual [M, K] of dx's type, or NULL; it may be dx itself.
+ *   dx       [M, K], bf16 or fp32.
+ * FT_ERR_UNSUPPORTED: N > 65536, K > 2^20, N K / 2, or M N / 32 from 2 GiB on.
+ */
+ft_status ft_linear8_bwd_input(const uint8_t *gq, const uint8_t *gs, int64_t M, int64_t N, const uint8_t *wq,
+                               const uint8_t *ws, int64_t K, const float *Qp, int32_t R, const void *D, const void *z,
+                               ft_act act, const void *residual, void *dx, ft_dtype dx_dtype, hipStream_t stream);
+
 /* Static description of a status code. */
 const char *ft_status_string(ft_status status);
 

@@ -24,6 +24,7 @@ EXPORTED = ("ft_quantize_blockwise", "ft_linear_fwd", "ft_linear_bwd_input", "ft
 
 FT_SCALE_FLOOR, FT_SCALE_NO_CLIP = 0, 1
 FT_ROUND_NEAREST_EVEN, FT_ROUND_STOCHASTIC = 0, 1
+FT_ACT_NONE, FT_ACT_GELU, FT_ACT_SILU, FT_ACT_RELU = range(4)
 
 
 class QuantMode(ctypes.Structure):
@@ -94,6 +95,19 @@ def load():
         L.ft_linear_bwd_input_dgelu.restype = ctypes.c_int
         L.ft_linear_bwd_input_dgelu_workspace_size.argtypes = [_I64, _I64, _I32]
         L.ft_linear_bwd_input_dgelu_workspace_size.restype = _Z
+        L.ft_rmsnorm_quantize8.argtypes = [_P, _P, _P, _I64, _I64, ctypes.c_float, _P, _P, _P, _P, _P, _P]
+        L.ft_rmsnorm_bwd.argtypes = [_P, _P, _P, _P, _P, _I64, _I64, _P, _P, _P, _Z, _P]
+        L.ft_rmsnorm_bwd_workspace_size.argtypes = [_I64, _I64]
+        L.ft_rmsnorm_bwd_workspace_size.restype = _Z
+        L.ft_quantize8.argtypes = [_P, _P, ctypes.c_int, _I64, _I64, _P, _P, _P, _P, _I32, ctypes.c_int, _P, _P, _Z, _P]
+        L.ft_quantize8_workspace_size.argtypes = [_I64, _I64, _I32, ctypes.c_int]
+        L.ft_quantize8_workspace_size.restype = _Z
+        L.ft_linear8_fwd.argtypes = [_P, _P, _I64, _I64, _P, _P, _I64, _P, _I32, _P, _P, ctypes.c_int, _P, _P, _P,
+                                     ctypes.c_int, _P]
+        L.ft_linear8_bwd_input.argtypes = [_P, _P, _I64, _I64, _P, _P, _I64, _P, _I32, _P, _P, ctypes.c_int, _P, _P,
+                                           ctypes.c_int, _P]
+        for f in ("ft_rmsnorm_quantize8", "ft_rmsnorm_bwd", "ft_quantize8", "ft_linear8_fwd", "ft_linear8_bwd_input"):
+            getattr(L, f).restype = ctypes.c_int
         for f in ("ft_quantize_blockwise", "ft_linear_fwd", "ft_linear_bwd_input", "ft_lora_grads"):
             getattr(L, f).restype = ctypes.c_int
         L.ft_status_string.argtypes = [ctypes.c_int]
@@ -500,4 +514,199 @@ def ft_linear_bwd_input_nvfp4(gq, gs, gt, wq, ws, wt, K):
     dx = torch.empty((M, K), dtype=torch.float32, device=dev)
     _check(L.ft_linear_bwd_input_nvfp4(_ptr(gq), _ptr(gs), _ptr(gt), M, N, _ptr(wq), _ptr(ws), _ptr(wt), K, _ptr(dx),
                                        _stream(dev)))
+    return dx
+
+
+# ------------------------------------------------ 8-bit activations and gradients
+F8 = torch.float8_e4m3fn
+
+
+def _launch(f, dev, *args):
+    """f on this device's current stream."""
+    if torch.cuda.current_device() == dev.index:
+        _check(f(*args, _stream(dev)))
+    else:
+        with torch.cuda.device(dev):
+            _check(f(*args, _stream(dev)))
+
+
+def _like(t, name, shape, dtype, dev):
+    """The caller's output (checked) or a new one."""
+    if t is None:
+        return torch.empty(shape, dtype=dtype, device=dev)
+    _need(t, name, dtype, dev)
+    if t.shape != shape:
+        raise ValueError("%s must be %s, got %s" % (name, tuple(shape), tuple(t.shape)))
+    return t
+
+
+def _opt(t, name, shape, dtype, dev):
+    """An optional input (checked)."""
+    return None if t is None else _like(t, name, shape, dtype, dev)
+
+
+def scales8_shape(rows, cols):
+    """Shape of the E8M0 scales of MXFP8 [rows, cols]: block 4 g + j of row m at [g, m, j]."""
+    return ((cols + 127) // 128, rows, 4)
+
+
+def ft_rmsnorm_quantize8(x, w, residual=None, eps=1e-6, h=None, y=None, codes=None, scales=None, rstd=None,
+                         want_y=False, want_codes=True, want_rstd=False):
+    """RMS norm of h = x + residual with an MXFP8 output.
+
+    x, residual bf16 [rows, cols], w bf16 [cols].  Returns (h, y, codes, scales,
+    rstd): h bf16 (x itself without a residual; it may be x or residual, updated
+    in place), y = h / rms(h) * w in bf16 or None, codes float8_e4m3fn and scales
+    uint8 (E8M0) [ceil(cols / 128), rows, 4] of the unrounded y or None, rstd
+    fp32 [rows] or None.  y, codes and rstd are made where an output is passed or
+    asked for.
+    """
+    L = load()
+    _need(x, "x", torch.bfloat16, ndim=2)
+    dev, (rows, cols) = x.device, x.shape
+    _need(w, "w", torch.bfloat16, dev, ndim=1)
+    if w.shape[0] != cols:
+        raise ValueError("w must be [%d]" % cols)
+    if residual is not None:
+        _like(residual, "residual", x.shape, torch.bfloat16, dev)
+        h = _like(h, "h", x.shape, torch.bfloat16, dev)
+    elif h is not None:
+        raise ValueError("h goes with a residual")
+    if y is not None or want_y:
+        y = _like(y, "y", x.shape, torch.bfloat16, dev)
+    if codes is not None or scales is not None or want_codes:
+        codes = _like(codes, "codes", x.shape, F8, dev)
+        scales = _like(scales, "scales", scales8_shape(rows, cols), torch.uint8, dev)
+    if rstd is not None or want_rstd:
+        rstd = _like(rstd, "rstd", (rows,), torch.float32, dev)
+    _launch(L.ft_rmsnorm_quantize8, dev, _ptr(x), _ptr(residual), _ptr(w), rows, cols, eps, _ptr(h), _ptr(y), _ptr(codes),
+            _ptr(scales), _ptr(rstd))
+    return (x if residual is None else h), y, codes, scales, rstd
+
+
+def ft_rmsnorm_bwd(dy, h, w, rstd, dh=None, dx=None, dw=None, want_dw=True, workspace=None):
+    """Gradients of ft_rmsnorm_quantize8's y: (dx bf16 [rows, cols], of x and of
+    the residual alike, dw fp32 [cols] or None).  dh: the gradient that reaches h
+    on the residual stream; dx may be dy or dh."""
+    L = load()
+    _need(dy, "dy", torch.bfloat16, ndim=2)
+    dev, (rows, cols) = dy.device, dy.shape
+    _like(h, "h", dy.shape, torch.bfloat16, dev)
+    _like(w, "w", (cols,), torch.bfloat16, dev)
+    _like(rstd, "rstd", (rows,), torch.float32, dev)
+    _opt(dh, "dh", dy.shape, torch.bfloat16, dev)
+    dx = _like(dx, "dx", dy.shape, torch.bfloat16, dev)
+    if dw is not None or want_dw:
+        dw = _like(dw, "dw", (cols,), torch.float32, dev)
+        workspace = _workspace(L.ft_rmsnorm_bwd_workspace_size(rows, cols), dev, workspace)
+    _launch(L.ft_rmsnorm_bwd, dev, _ptr(dy), _ptr(dh), _ptr(h), _ptr(w), _ptr(rstd), rows, cols, _ptr(dx), _ptr(dw),
+            _ptr(workspace), _nbytes(workspace))
+    return dx, dw
+
+
+def ft_rmsnorm_bwd_workspace_size(rows, cols):
+    return int(load().ft_rmsnorm_bwd_workspace_size(rows, cols))
+
+
+def ft_quantize8(src, z=None, act=FT_ACT_NONE, proj=None, proj_layout=FT_PROJ_COLS_BY_R, v=None, codes=None, scales=None,
+                 proj_out=None, want_v=True, workspace=None):
+    """MXFP8 of bf16 src [rows, cols]: (codes float8_e4m3fn, scales uint8
+    [ceil(cols / 128), rows, 4], proj_out fp32 [rows, R] or None, v).
+
+    With proj, also src . proj as ft_quantize_blockwise.  With z and act, what is
+    quantized is src * act'(z), which v holds in bf16 (None without want_v; v may
+    be src).
+    """
+    L = load()
+    _need(src, "src", torch.bfloat16, ndim=2)
+    dev, (rows, cols) = src.device, src.shape
+    codes = _like(codes, "codes", src.shape, F8, dev)
+    scales = _like(scales, "scales", scales8_shape(rows, cols), torch.uint8, dev)
+    _opt(z, "z", src.shape, torch.bfloat16, dev)
+    if z is not None and (v is not None or want_v):
+        v = _like(v, "v", src.shape, torch.bfloat16, dev)
+    R = 0
+    if proj is not None:
+        _need(proj, "proj", torch.bfloat16, dev, ndim=2)
+        R, other = proj.shape if proj_layout == FT_PROJ_R_BY_COLS else proj.shape[::-1]
+        if other != cols:
+            raise ValueError("proj shape %s does not match cols %d" % (tuple(proj.shape), cols))
+        proj_out = _like(proj_out, "proj_out", (rows, R), torch.float32, dev)
+        workspace = _workspace(L.ft_quantize8_workspace_size(rows, cols, R, proj_layout), dev, workspace)
+    else:
+        proj_out = None
+    _launch(L.ft_quantize8, dev, _ptr(src), _ptr(z), act, rows, cols, _ptr(v), _ptr(codes), _ptr(scales), _ptr(proj), R,
+            proj_layout, _ptr(proj_out), _ptr(workspace), _nbytes(workspace))
+    return codes, scales, proj_out, v
+
+
+def ft_quantize8_workspace_size(rows, cols, R=0, proj_layout=FT_PROJ_COLS_BY_R):
+    return int(load().ft_quantize8_workspace_size(rows, cols, R, proj_layout))
+
+
+def _linear8_operands(q, s, wq, ws, reduce_rows):
+    """(device, M, N, K) of an 8-bit product; reduce_rows: over the weight's rows N (the backward)."""
+    _need(q, "codes", F8, ndim=2)
+    dev = q.device
+    _need(wq, "wq", torch.uint8, dev, ndim=2)
+    _need(ws, "ws", torch.uint8, dev)
+    M, N, K = q.shape[0], wq.shape[0], 2 * wq.shape[1]
+    if q.shape[1] != (N if reduce_rows else K) or ws.numel() * 1024 != N * K:
+        raise ValueError("operand shapes do not match: codes %s, wq %s, ws %s" % (tuple(q.shape), tuple(wq.shape),
+                                                                               tuple(ws.shape)))
+    _like(s, "scales", scales8_shape(M, q.shape[1]), torch.uint8, dev)
+    return dev, M, N, K
+
+
+def _output8(out, name, shape, out_dtype, dev):
+    dt = out_dtype if out is None else out.dtype
+    if dt not in (torch.bfloat16, torch.float32):
+        raise ValueError("%s must be bf16 or fp32" % name)
+    return _like(out, name, shape, dt, dev)
+
+
+def ft_linear8_fwd(xq, xs, wq, ws, P=None, U=None, bias=None, act=FT_ACT_NONE, residual=None, out_dtype=torch.bfloat16,
+                   z=None, want_z=False, y=None):
+    """y [M, N] = act(DQ(xq) DQ(wq)^T + P U + bias) + residual on MXFP8
+    activations (xq float8_e4m3fn [M, K], xs uint8 [ceil(K / 128), M, 4]).
+    residual has y's type and may be y.  Returns y, or (y, z) with z, act's input
+    in bf16, where z is passed or asked for."""
+    L = load()
+    dev, M, N, K = _linear8_operands(xq, xs, wq, ws, False)
+    R = 0
+    if P is not None or U is not None:
+        _need(P, "P", torch.float32, dev, ndim=2)
+        R = P.shape[1]
+        _like(P, "P", (M, R), torch.float32, dev)
+        _need(U, "U", torch.bfloat16, dev)
+        _like(U, "U", (R, N), torch.bfloat16, dev)
+    _opt(bias, "bias", (N,), torch.bfloat16, dev)
+    y = _output8(y, "y", (M, N), out_dtype, dev)
+    _opt(residual, "residual", (M, N), y.dtype, dev)
+    if z is not None or want_z:
+        z = _like(z, "z", (M, N), torch.bfloat16, dev)
+    _launch(L.ft_linear8_fwd, dev, _ptr(xq), _ptr(xs), M, K, _ptr(wq), _ptr(ws), N, _ptr(P), R, _ptr(U), _ptr(bias), act,
+            _ptr(residual), _ptr(z), _ptr(y), FT_F32 if y.dtype == torch.float32 else FT_BF16)
+    return y if z is None else (y, z)
+
+
+def ft_linear8_bwd_input(gq, gs, wq, ws, Qp=None, D=None, z=None, act=FT_ACT_NONE, residual=None,
+                         out_dtype=torch.bfloat16, dx=None):
+    """dx [M, K] = (DQ(gq) DQ(wq) + Qp D^T) * act'(z) + residual on MXFP8
+    gradients; z [M, K] bf16 is the saved input of the activation in front of the
+    layer, residual has dx's type and may be dx."""
+    L = load()
+    dev, M, N, K = _linear8_operands(gq, gs, wq, ws, True)
+    R = 0
+    if Qp is not None or D is not None:
+        _need(Qp, "Qp", torch.float32, dev, ndim=2)
+        R = Qp.shape[1]
+        _like(Qp, "Qp", (M, R), torch.float32, dev)
+        _need(D, "D", torch.bfloat16, dev)
+        _like(D, "D", (K, R), torch.bfloat16, dev)
+    _opt(z, "z", (M, K), torch.bfloat16, dev)
+    dx = _output8(dx, "dx", (M, K), out_dtype, dev)
+    _opt(residual, "residual", (M, K), dx.dtype, dev)
+    _launch(L.ft_linear8_bwd_input, dev, _ptr(gq), _ptr(gs), M, N, _ptr(wq), _ptr(ws), K, _ptr(Qp), R, _ptr(D), _ptr(z),
+            act, _ptr(residual), _ptr(dx), FT_F32 if dx.dtype == torch.float32 else FT_BF16)
     return dx

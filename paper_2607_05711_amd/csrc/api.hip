@@ -267,7 +267,7 @@ ft_status ft_linear_bwd_input_dgelu(const uint8_t* gq, const uint8_t* gs, int64_
   return hip_status(R1 == 0 ? ft::launch_quant_rows((const uint16_t*)dz, (int)M, (int)K, dzq, dzs, nullptr, 0, 0, nullptr,
                                                     nullptr, stream)
                             : ft::launch_quant_proj((const uint16_t*)dz, (int)M, (int)K, dzq, dzs, (const uint16_t*)U1, R1,
-                                                    FT_PROJ_R_BY_COLS, false, Qp1, (float*)workspace,
+                                                    FT_PROJ_R_BY_COLS, 0, Qp1, (float*)workspace,
                                                     ft::gemm_fp4_col_tiles((int)K), kMlpChain, nullptr, stream),
                     "linear bwd input dgelu (quantize)");
 }
@@ -381,10 +381,153 @@ ft_status ft_linear_bwd_input_nvfp4(const uint8_t* gq, const uint8_t* gs, const 
   return nvfp4_gemm(true, gq, gs, gt, M, N, wq, ws, wt, K, dx, stream);
 }
 
+// ---- 8-bit activations and gradients
+
+static ft_status check_act(ft_act act) {
+  if (act != FT_ACT_NONE && act != FT_ACT_GELU && act != FT_ACT_SILU && act != FT_ACT_RELU)
+    return fail(FT_ERR_UNSUPPORTED, "act = %d", (int)act);
+  return FT_OK;
+}
+
+constexpr int64_t kNormCols = 16384;
+
+ft_status ft_rmsnorm_quantize8(const void* x, const void* residual, const void* w, int64_t rows, int64_t cols, float eps,
+                               void* h, void* y, uint8_t* codes, uint8_t* scales, float* rstd, hipStream_t stream) {
+  g_last_error[0] = 0;
+  FT_TRY(check_dim("rows", rows, 1));
+  FT_TRY(check_dim("cols", cols, 32));
+  if (cols > kNormCols) return fail(FT_ERR_UNSUPPORTED, "cols = %lld: at most %lld", (long long)cols, (long long)kNormCols);
+  if (!(eps >= 0.0f)) return fail(FT_ERR_UNSUPPORTED, "eps = %g", (double)eps);
+  if (!residual != !h) return fail(FT_ERR_UNSUPPORTED, "h goes with a residual");
+  if (!codes != !scales) return fail(FT_ERR_NULL, "codes and scales go together");
+  if (rows == 0 || cols == 0) return FT_OK;
+  if (!x || !w || (!y && !codes)) return fail(FT_ERR_NULL, "x, w, and y or codes are required");
+  if (!aligned16(x) || !aligned16(residual) || !aligned16(w) || !aligned16(h) || !aligned16(y) || !aligned16(codes) ||
+      !aligned16(scales) || !aligned16(rstd))
+    return fail(FT_ERR_ALIGN, "x, residual, w, h, y, codes, scales, rstd must be 16-byte aligned");
+  return hip_status(ft::launch_rmsnorm_q8((const uint16_t*)x, (const uint16_t*)residual, (const uint16_t*)w, eps,
+                                          (int)rows, (int)cols, (uint16_t*)h, (uint16_t*)y, codes, scales, rstd, stream),
+                    "rmsnorm quantize8");
+}
+
+size_t ft_rmsnorm_bwd_workspace_size(int64_t rows, int64_t cols) {
+  if (rows <= 0 || cols <= 0 || rows > kMaxDim || cols > kNormCols) return 0;
+  return ft::rmsnorm_bwd_workspace((int)rows, (int)cols);
+}
+
+ft_status ft_rmsnorm_bwd(const void* dy, const void* dh, const void* h, const void* w, const float* rstd, int64_t rows,
+                         int64_t cols, void* dx, float* dw, void* workspace, size_t workspace_bytes, hipStream_t stream) {
+  g_last_error[0] = 0;
+  FT_TRY(check_dim("rows", rows, 1));
+  FT_TRY(check_dim("cols", cols, 32));
+  if (cols > kNormCols) return fail(FT_ERR_UNSUPPORTED, "cols = %lld: at most %lld", (long long)cols, (long long)kNormCols);
+  if (cols == 0 || (rows == 0 && !dw)) return FT_OK;
+  if (rows > 0 && (!dy || !h || !w || !rstd || !dx)) return fail(FT_ERR_NULL, "dy, h, w, rstd and dx are required");
+  if (!aligned16(dy) || !aligned16(dh) || !aligned16(h) || !aligned16(w) || !aligned16(rstd) || !aligned16(dx) || !aligned16(dw))
+    return fail(FT_ERR_ALIGN, "dy, dh, h, w, rstd, dx, dw must be 16-byte aligned");
+  if (dw) FT_TRY(check_workspace(workspace, workspace_bytes, ft_rmsnorm_bwd_workspace_size(rows, cols)));
+  return hip_status(ft::launch_rmsnorm_bwd((const uint16_t*)dy, (const uint16_t*)dh, (const uint16_t*)h, (const uint16_t*)w,
+                                           rstd, (int)rows, (int)cols, (uint16_t*)dx, dw, (float*)workspace, stream),
+                    "rmsnorm bwd");
+}
+
+size_t ft_quantize8_workspace_size(int64_t rows, int64_t cols, int32_t R, ft_proj_layout proj_layout) {
+  if (R <= 0 || R > 128 || rows <= 0 || cols <= 0 || rows > kMaxDim || cols > (1 << 20)) return 0;
+  return ft::quant8_proj_workspace((int)rows, (int)cols, R, (int)proj_layout);
+}
+
+ft_status ft_quantize8(const void* src, const void* z, ft_act act, int64_t rows, int64_t cols, void* v, uint8_t* codes,
+                       uint8_t* scales, const void* proj, int32_t R, ft_proj_layout proj_layout, float* proj_out,
+                       void* workspace, size_t workspace_bytes, hipStream_t stream) {
+  g_last_error[0] = 0;
+  FT_TRY(check_dim("rows", rows, 1));
+  FT_TRY(check_dim("cols", cols, 32));
+  if (cols > (1 << 20)) return fail(FT_ERR_UNSUPPORTED, "cols = %lld: at most 2^20", (long long)cols);
+  FT_TRY(check_act(act));
+  if (!z != (act == FT_ACT_NONE) || (!z && v)) return fail(FT_ERR_UNSUPPORTED, "z goes with an activation, and v with z");
+  if (proj_layout != FT_PROJ_COLS_BY_R && proj_layout != FT_PROJ_R_BY_COLS)
+    return fail(FT_ERR_UNSUPPORTED, "proj_layout = %d", (int)proj_layout);
+  if (rows == 0 || cols == 0) return FT_OK;
+  if (!src || !codes || !scales) return fail(FT_ERR_NULL, "src, codes and scales are required");
+  if (!aligned16(src) || !aligned16(z) || !aligned16(v) || !aligned16(codes) || !aligned16(scales))
+    return fail(FT_ERR_ALIGN, "src, z, v, codes and scales must be 16-byte aligned");
+  FT_TRY(check_rank(R, proj, proj_out, "proj", "proj_out"));
+  if (R == 0)
+    return hip_status(ft::launch_quant8((const uint16_t*)src, (const uint16_t*)z, (int)act, (int)rows, (int)cols,
+                                        (uint16_t*)v, codes, scales, stream),
+                      "quantize8");
+  if (z) return fail(FT_ERR_UNSUPPORTED, "a projection of src * act'(z): quantize v");
+  FT_TRY(check_workspace(workspace, workspace_bytes, ft::quant8_proj_workspace((int)rows, (int)cols, R, (int)proj_layout)));
+  return hip_status(ft::launch_quant8_proj((const uint16_t*)src, (int)rows, (int)cols, codes, scales, (const uint16_t*)proj,
+                                           R, (int)proj_layout, proj_out, (float*)workspace, stream),
+                    "quantize8 with projection");
+}
+
+// tile: 0 for the rules' choice, else that output tile (see gemm_mx8_tile) or 1 for the kernel of few rows.
+static ft_status linear8(bool bwd, int tile, const uint8_t* x, const uint8_t* xs, int64_t M, int64_t N, int64_t K, const uint8_t* wq,
+                         const uint8_t* ws, const float* P, int32_t R, const void* lr, const void* bias, ft_act act,
+                         const void* residual, void* z, void* out, ft_dtype dtype, hipStream_t stream) {
+  g_last_error[0] = 0;
+  FT_TRY(check_dim("M", M, 1));
+  FT_TRY(check_dim("N", N, 32));
+  FT_TRY(check_dim("K", K, 32));
+  if (dtype != FT_BF16 && dtype != FT_F32) return fail(FT_ERR_UNSUPPORTED, "output dtype = %d", (int)dtype);
+  FT_TRY(check_act(act));
+  if (bwd && !z != (act == FT_ACT_NONE)) return fail(FT_ERR_UNSUPPORTED, "z goes with an activation");
+  if (M == 0 || (bwd ? K : N) == 0) return FT_OK;
+  if ((bwd ? N : K) == 0) return fail(FT_ERR_SHAPE, "empty reduction");
+  if (!x || !xs || !wq || !ws || !out) return fail(FT_ERR_NULL, "codes, scales and the output are required");
+  if (!aligned16(x) || !aligned16(xs) || !aligned16(wq) || !aligned16(ws) || !aligned16(out) || !aligned16(bias) ||
+      !aligned16(residual) || !aligned16(z))
+    return fail(FT_ERR_ALIGN, "codes, scales, bias, residual, z and the output must be 16-byte aligned");
+  FT_TRY(check_rank(R, P, lr, bwd ? "Qp" : "P", bwd ? "D" : "U"));
+  if (!ft::gemm_mx8_supported(bwd, (int)M, (int)N, (int)K, R))
+    return fail(FT_ERR_UNSUPPORTED, "M = %lld, N = %lld, K = %lld: operands too large for 32-bit offsets", (long long)M,
+                (long long)N, (long long)K);
+  if (tile == 0)
+    tile = !bwd && ft::rows_mx8_better((int)M, (int)N, (int)K) ? 1 : ft::gemm_mx8_tile(bwd, (int)M, (int)N, (int)K);
+  const ft::MxArgs a{x, xs, wq, ws, (int)M, (int)N, (int)K, P, R, (const uint16_t*)lr, (const uint16_t*)bias, (uint16_t*)z,
+                     residual, out};
+  if (tile == 1) return hip_status(ft::launch_rows_mx8(a, (int)act, dtype == FT_F32, stream), "linear8 fwd (few rows)");
+  return hip_status(ft::launch_gemm_mx8(bwd, tile, a, (int)act, dtype == FT_F32, stream),
+                    bwd ? "linear8 bwd input" : "linear8 fwd");
+}
+
+ft_status ft_linear8_fwd(const uint8_t* xq, const uint8_t* xs, int64_t M, int64_t K, const uint8_t* wq, const uint8_t* ws,
+                         int64_t N, const float* P, int32_t R, const void* U, const void* bias, ft_act act,
+                         const void* residual, void* z, void* y, ft_dtype y_dtype, hipStream_t stream) {
+  return linear8(false, 0, xq, xs, M, N, K, wq, ws, P, R, U, bias, act, residual, z, y, y_dtype, stream);
+}
+
+ft_status ft_linear8_bwd_input(const uint8_t* gq, const uint8_t* gs, int64_t M, int64_t N, const uint8_t* wq,
+                               const uint8_t* ws, int64_t K, const float* Qp, int32_t R, const void* D, const void* z,
+                               ft_act act, const void* residual, void* dx, ft_dtype dx_dtype, hipStream_t stream) {
+  return linear8(true, 0, gq, gs, M, N, K, wq, ws, Qp, R, D, nullptr, act, residual, const_cast<void*>(z), dx, dx_dtype,
+                 stream);
+}
+
 // Which kernel a product runs on (see gemm_fp4_kernel): for the tests of the
 // dispatch, not part of the public header.
 int ftx_gemm_kernel(int bwd, int64_t M, int64_t N, int64_t K, int32_t R, int out_f32) {
   return ft::gemm_fp4_kernel(bwd != 0, (int)M, (int)N, (int)K, R, out_f32 != 0);
+}
+// What a call of the 8-bit linear runs on, and the call on a kernel of the tests' choosing.
+int ftx_linear8_tile(int bwd, int64_t M, int64_t N, int64_t K) {
+  return !bwd && ft::rows_mx8_better((int)M, (int)N, (int)K) ? 1 : ft::gemm_mx8_tile(bwd != 0, (int)M, (int)N, (int)K);
+}
+ft_status ftx_linear8_fwd(int tile, const uint8_t* xq, const uint8_t* xs, int64_t M, int64_t K, const uint8_t* wq,
+                          const uint8_t* ws, int64_t N, const float* P, int32_t R, const void* U, const void* bias,
+                          ft_act act, const void* residual, void* z, void* y, ft_dtype y_dtype, hipStream_t stream) {
+  if (tile != 64 && tile != 128 && tile != 256 && !(tile == 1 && M <= ft::kRowsMx8Max))
+    return fail(FT_ERR_UNSUPPORTED, "tile = %d", tile);
+  return linear8(false, tile, xq, xs, M, N, K, wq, ws, P, R, U, bias, act, residual, z, y, y_dtype, stream);
+}
+ft_status ftx_linear8_bwd_input(int tile, const uint8_t* gq, const uint8_t* gs, int64_t M, int64_t N, const uint8_t* wq,
+                                const uint8_t* ws, int64_t K, const float* Qp, int32_t R, const void* D, const void* z,
+                                ft_act act, const void* residual, void* dx, ft_dtype dx_dtype, hipStream_t stream) {
+  if (tile != 64 && tile != 128 && tile != 256) return fail(FT_ERR_UNSUPPORTED, "tile = %d", tile);
+  return linear8(true, tile, gq, gs, M, N, K, wq, ws, Qp, R, D, nullptr, act, residual, const_cast<void*>(z), dx, dx_dtype,
+                 stream);
 }
 // Roundings of a projection's sum in the streaming quantize kernel, and in
 // max_groups partials of the chunked kernel.

@@ -10,6 +10,12 @@
 //     C/D: column l%32, rows 8*(v/4) + 4*(l/32) + v%4 for v = 0..15.
 //   v_mfma_f32_32x32x16_bf16: A row l%32 / B column l%32, reduction
 //     elements [8*(l/32), +8); C/D as above.
+//   The same instruction with FP8 B (E4M3): a lane's 32 bytes are the reduction
+//     elements [16*(l/32), +16) and [32 + 16*(l/32), +16), while its scale byte
+//     is that of the contiguous block [32*(l/32), +32), as with FP4.
+//   v_mfma_scale_f32_16x16x128_f8f6f4: row or column l%16; FP4 elements
+//     [32*(l/16), +32), FP8 elements [16*(l/16), +16) and [64 + 16*(l/16), +16),
+//     scale byte of block 32*(l/16); C/D: column l%16, rows 4*(l/16) + v.
 //   ds_read_b64_tr_b4: in each 16-lane group lane s supplies the address of
 //     16 nibbles (a row); lane c receives nibble c of rows 0..15, in order.
 //   ds_read_b64_tr_b16: in each 16-lane group, output lane i element j is
@@ -17,12 +23,14 @@
 #pragma once
 #include <hip/hip_runtime.h>
 #include <stdint.h>
+#include <type_traits>
 
 namespace ft {
 
 typedef int v2i __attribute__((ext_vector_type(2)));
 typedef int v4i __attribute__((ext_vector_type(4)));
 typedef int v8i __attribute__((ext_vector_type(8)));
+typedef short v2s __attribute__((ext_vector_type(2)));
 typedef short v4s __attribute__((ext_vector_type(4)));
 typedef float v16f __attribute__((ext_vector_type(16)));
 typedef __bf16 v8bf __attribute__((ext_vector_type(8)));
@@ -74,8 +82,9 @@ __device__ __forceinline__ uint32_t e8m0_noclip_from_amax_bits(uint32_t amax_bit
 }
 
 // Numerics mode of the 1x32 quantizers (a template argument): bit 0 selects
-// the no-clip scale rule, bit 1 stochastic rounding.
-enum { QM_NOCLIP = 1, QM_SR = 2 };
+// the no-clip scale rule, bit 1 stochastic rounding, bit 2 MXFP8 (the streaming
+// kernel only).
+enum { QM_NOCLIP = 1, QM_SR = 2, QM_E4M3 = 4 };
 
 template <int QM>
 __device__ __forceinline__ uint32_t e8m0_of(uint32_t amax_bits) {
@@ -167,6 +176,124 @@ __device__ __forceinline__ float gelu_tanh_grad(float z) {
   const float e = __builtin_amdgcn_exp2f(z * fmaf(kGeluB, t, kGeluA));
   const float r = __builtin_amdgcn_rcpf(1.0f + e);
   return fmaf(z * fmaf(kGeluG3, t, kGeluG1) * (1.0f - r), r, r);
+}
+
+// SiLU(z) = z r with r = 1 / (1 + exp(-z)), and SiLU'(z) = r + z r (1 - r), on the
+// hardware exp2 and reciprocal (1 ulp each) like the GELU above.
+__device__ __forceinline__ float silu_r(float z) {
+  return __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(-1.4426950408889634f * z));
+}
+
+// Activations of the 8-bit linear's epilogue (ft_act), act(z) and act'(z) in fp32.
+enum { ACT_NONE = 0, ACT_GELU = 1, ACT_SILU = 2, ACT_RELU = 3 };
+template <int ACT>
+__device__ __forceinline__ float act_fn(float z) {
+  if constexpr (ACT == ACT_GELU) return gelu_tanh(z);
+  else if constexpr (ACT == ACT_SILU) return z * silu_r(z);
+  else if constexpr (ACT == ACT_RELU) return z < 0.0f ? 0.0f : z;   // keeps a NaN
+  else return z;
+}
+template <int ACT>
+__device__ __forceinline__ float act_grad(float z) {
+  if constexpr (ACT == ACT_GELU) {
+    // 0 or 1 to fp32 past 16, where z^3 may pass fp32's range (a NaN stays one)
+    return gelu_tanh_grad(z > 16.0f ? 16.0f : z < -16.0f ? -16.0f : z);
+  } else if constexpr (ACT == ACT_SILU) {
+    const float r = silu_r(z);
+    return fmaf(z * r, 1.0f - r, r);
+  } else if constexpr (ACT == ACT_RELU) {
+    return z > 0.0f ? 1.0f : 0.0f;
+  } else {
+    return 1.0f;
+  }
+}
+
+// MXFP8 (E4M3 elements): the E8M0 code of the smallest e with amax / 2^e <= 448.
+// With amax = m 2^E, m in [1, 2): E - 8, one more where m > 1.75 (448 = 1.75
+// 2^8), clamped at code 0.  So nothing saturates: the floor rule of the FP4
+// blocks would clip a block's largest element by up to 1/8, twice an E4M3
+// rounding.  An infinity or NaN in the block gives 255, the E8M0 NaN, which
+// makes the whole block NaN wherever it is read.
+__device__ __forceinline__ uint32_t e8m0_e4m3_from_f32(uint32_t amax_bits) {
+  const int e = (int)(amax_bits >> 23) - 8 + ((amax_bits & 0x7FFFFFu) > 0x600000u ? 1 : 0);
+  return amax_bits >= 0x7F800000u ? 255u : (uint32_t)max(e, 0);
+}
+__device__ __forceinline__ uint32_t e8m0_e4m3_from_bf16(uint32_t amax_bits) { return e8m0_e4m3_from_f32(amax_bits << 16); }
+
+// max over the 4 lanes of each aligned quad
+__device__ __forceinline__ uint32_t quad_max(uint32_t m) {
+  m = max(m, (uint32_t)__builtin_amdgcn_mov_dpp((int)m, 0xB1, 0xF, 0xF, true));  // quad_perm [1,0,3,2]
+  m = max(m, (uint32_t)__builtin_amdgcn_mov_dpp((int)m, 0x4E, 0xF, 0xF, true));  // quad_perm [2,3,0,1]
+  return m;
+}
+
+// 8 consecutive fp32 of a 32-element block held by a lane quad, in MXFP8: the 8
+// bytes, and the block's E8M0 code.  One rounding, from fp32, to nearest even.
+__device__ __forceinline__ v2i quad_mxfp8(const float (&f)[8], uint32_t& scale_code) {
+  uint32_t m = 0;
+#pragma unroll
+  for (int e = 0; e < 8; e++) m = max(m, __float_as_uint(f[e]) & 0x7FFFFFFFu);
+  scale_code = e8m0_e4m3_from_f32(quad_max(m));
+  const float s = e8m0_to_f32(scale_code);
+  v2i o;
+#pragma unroll
+  for (int e = 0; e < 2; e++) {
+    v2s q = {0, 0};
+    q = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(q, f[4 * e], f[4 * e + 1], s, false);
+    q = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(q, f[4 * e + 2], f[4 * e + 3], s, true);
+    o[e] = __builtin_bit_cast(int, q);
+  }
+  return o;
+}
+
+// E4M3 bytes of x with magnitude 2 or more (bit 6 set) stay in x, the others move to low.
+__device__ __forceinline__ void split_e4m3(v8i& x, v8i& low) {
+#pragma unroll
+  for (int e = 0; e < 8; e++) {
+    const uint32_t b = ((uint32_t)x[e] >> 6) & 0x01010101u, m = (b << 8) - b;   // 0xFF in those bytes
+    low[e] = x[e] & (int)~m;
+    x[e] &= (int)m;
+  }
+}
+
+// The four quads of a 16-lane row hold one byte each: all four as a dword.
+__device__ __forceinline__ uint32_t row_bytes(uint32_t byte, int lane) {
+  uint32_t d = byte << (8 * ((lane >> 2) & 3));
+  d |= (uint32_t)__builtin_amdgcn_mov_dpp((int)d, 0x124, 0xF, 0xF, true);                // row_ror:4
+  return d | (uint32_t)__builtin_amdgcn_mov_dpp((int)d, 0x128, 0xF, 0xF, true);          // row_ror:8
+}
+
+// Sum over the wave, the same bits in every lane (each step adds a lane and its mirror image).
+__device__ __forceinline__ float wave_sum(float x) {
+  const auto dpp = [](float v, auto ctl) {
+    return __int_as_float(__builtin_amdgcn_mov_dpp(__float_as_int(v), decltype(ctl)::value, 0xF, 0xF, true));
+  };
+  x += dpp(x, std::integral_constant<int, 0xB1>{});
+  x += dpp(x, std::integral_constant<int, 0x4E>{});
+  x += dpp(x, std::integral_constant<int, 0x141>{});   // row_half_mirror
+  x += dpp(x, std::integral_constant<int, 0x140>{});   // row_mirror
+  const auto a = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  x = __uint_as_float(a[0]) + __uint_as_float(a[1]);
+  const auto b = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  return __uint_as_float(b[0]) + __uint_as_float(b[1]);
+}
+
+// 8 bf16 in 16 bytes, as fp32 and back (round to nearest even).
+__device__ __forceinline__ void unpack_bf16x8(v4i x, float (&f)[8]) {
+#pragma unroll
+  for (int e = 0; e < 4; e++) {
+    f[2 * e] = bf16_to_f32((uint32_t)x[e] & 0xFFFFu);
+    f[2 * e + 1] = __uint_as_float((uint32_t)x[e] & 0xFFFF0000u);
+  }
+}
+__device__ __forceinline__ v4i pack_bf16x8(const float (&f)[8]) {
+  v4i r;
+#pragma unroll
+  for (int e = 0; e < 4; e++) {
+    const v2f p = {f[2 * e], f[2 * e + 1]};
+    r[e] = (int)__builtin_bit_cast(uint32_t, __builtin_convertvector(p, v2bf));
+  }
+  return r;
 }
 
 // Quantize 8 consecutive bf16 (packed in w) of a 32-element block held by a

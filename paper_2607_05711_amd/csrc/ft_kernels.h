@@ -30,12 +30,13 @@ hipError_t launch_quant_gelu(const uint16_t* z, int rows, int cols, uint16_t* h,
                              hipStream_t st);
 // Streaming form of the row quantization with a projection (nearest-even
 // rounding): at most max_groups partials in ws, and no projection sum of more
-// roundings than max_groups partials of max_chain each.  gelu_out: src is z, h =
-// bf16(GELU(z)) is stored there and quantized (layout 0).
+// roundings than max_groups partials of max_chain each.  qm: 0, QM_NOCLIP or
+// QM_E4M3.  gelu_out: src is z, h = bf16(GELU(z)) is stored there and quantized
+// (layout 0).
 int quant_proj_steps(int rows, int cols, int R, int max_groups, int max_chain);
 bool quant_proj_supported(int rows, int cols, int R);
 hipError_t launch_quant_proj(const uint16_t* src, int rows, int cols, uint8_t* codes, uint8_t* scales,
-                             const uint16_t* proj, int R, int layout, bool no_clip, float* proj_out, float* ws,
+                             const uint16_t* proj, int R, int layout, int qm, float* proj_out, float* ws,
                              int max_groups, int max_chain, uint16_t* gelu_out, hipStream_t st);
 // Partials that the row quantization's workspace holds, and the products that
 // the chunked kernel adds into one of them.
@@ -89,6 +90,48 @@ hipError_t launch_gemm_fp4_fused(bool bwd, const uint8_t* a, const uint8_t* as, 
 // partials that their workspace holds.
 bool gemm_fp4_fused_supported(bool bwd, int M, int N, int K, int R, int R2);
 int gemm_fp4_col_tiles(int NO);
+
+// ---- 8-bit activations and gradients (MXFP8: E4M3, scales [cols / 128, rows, 4])
+// h = bf16(x + res) (res NULL: h is x and nothing is stored); y = h / rms(h) * w;
+// y, codes and scales, rstd: NULL for none.  K <= 16384, a multiple of 32.
+hipError_t launch_rmsnorm_q8(const uint16_t* x, const uint16_t* res, const uint16_t* w, float eps, int rows, int K,
+                             uint16_t* h, uint16_t* y, uint8_t* codes, uint8_t* scales, float* rstd, hipStream_t st);
+// dx = dh + its gradient; dw NULL for none, else ws holds rmsnorm_bwd_workspace bytes.
+size_t rmsnorm_bwd_workspace(int rows, int K);
+hipError_t launch_rmsnorm_bwd(const uint16_t* dy, const uint16_t* dh, const uint16_t* h, const uint16_t* w,
+                              const float* rstd, int rows, int K, uint16_t* dx, float* dw, float* ws, hipStream_t st);
+// MXFP8 of src, or of src act'(z) (z not NULL; bf16 of it stored in v).
+hipError_t launch_quant8(const uint16_t* src, const uint16_t* z, int act, int rows, int cols, uint16_t* v, uint8_t* codes,
+                         uint8_t* scales, hipStream_t st);
+
+// MXFP8 of src, with its product with proj (layout as in launch_quant_rows; ws holds quant8_proj_workspace bytes).
+size_t quant8_proj_workspace(int rows, int cols, int R, int layout);
+hipError_t launch_quant8_proj(const uint16_t* src, int rows, int cols, uint8_t* codes, uint8_t* scales,
+                              const uint16_t* proj, int R, int layout, float* proj_out, float* ws, hipStream_t st);
+
+// FP8 x FP4 GEMM with epilogue.  bwd = false: out[M, N] = act(X W^T + P U + bias) + res,
+// z (or NULL) receives act's input in bf16; bwd = true: out[M, K] = (X W + P D^T) act'(z) + res.
+struct MxArgs {
+  const uint8_t *x, *xs, *wq, *ws;
+  int M, N, K;
+  const float* P;
+  int R;
+  const uint16_t *lr, *bias;
+  uint16_t* z;
+  const void* res;
+  void* out;
+};
+bool gemm_mx8_supported(bool bwd, int M, int N, int K, int R);
+// Which output tile: 256 (256x256), 128 (128x128) or 64 (64x128).
+int gemm_mx8_tile(bool bwd, int M, int N, int K);
+hipError_t launch_gemm_mx8(bool bwd, int tile, const MxArgs& a, int act, bool out_f32, hipStream_t st);
+hipError_t launch_gemm_mx8_bf16(bool bwd, int tile, const MxArgs& a, int act, hipStream_t st);
+hipError_t launch_gemm_mx8_f32(bool bwd, int tile, const MxArgs& a, int act, hipStream_t st);
+
+// The forward over few rows (M <= kRowsMx8Max), and whether it is the faster one there.
+constexpr int kRowsMx8Max = 64;
+bool rows_mx8_better(int M, int N, int K);
+hipError_t launch_rows_mx8(const MxArgs& a, int act, bool out_f32, hipStream_t st);
 
 // Adapter gradients; token chunks leave partials in ws (lora_grads_workspace bytes).
 size_t lora_grads_workspace(int M, int K, int N, int ld, int r);

@@ -1,0 +1,520 @@
+// Block-scaled FP8 x FP4 GEMM (gfx950): 8-bit activations or gradients times
+// the frozen MXFP4 weight, with the low-rank term, bias, activation and
+// residual in the same kernel.
+//   forward   out[M, N] = act(X W^T + P U + bias) + residual       (z: act's input)
+//   backward  out[M, K] = (G W + Qp D^T) act'(z) + residual
+// X, G: E4M3, scales [reduction / 128, M, 4];  W: E2M1 codes [N, K / 2], scales
+// per 32 x 32 tile, read in transposed order by the backward.
+//
+// Workgroup: 4 waves in a 2x2 grid over a TM x TN tile of outputs, computed
+// transposed (the weight is MFMA operand A), so that a lane holds runs of four
+// columns of one output row.  Stages of 128 reduction elements (X: whole
+// 128-byte rows) move through an LDS ring of NS slots by buffer loads that
+// write LDS directly; the low-rank term is extra stages of the same ring (bf16
+// MFMAs, P split into bf16 terms).  A stage is two MFMA steps of 64: while
+// one step's products run, the other's fragments are read, one read per MFMA,
+// and the loads of the stage NS further go out behind the second step's.
+// The weight's scales of the whole reduction stay in LDS.
+//
+// An MFMA with an FP8 operand takes 64 cycles per wave and 32x32x64 products,
+// twice the FP4 time.  It adds its products in groups of eight consecutive
+// reduction elements, in which it drops what lies below 2^-14 of the largest
+// product's power of two; the groups' sums are added in fp32.  On ordinary
+// values that is an error of some 4e-6 of the result (2-norm), up to 3e-5 where
+// outlier channels share blocks with small values: far inside a bf16 result's
+// 2^-9, but not inside an fp32 one's.  F32 therefore splits X in two at |x| = 2
+// (bit 6 of the code) and makes two products: at or above 2, x's last place is
+// 2^-2 or more, so products are multiples of 2^-3, 2^-14 of the largest
+// possible, 448 * 6; below 2 they are multiples of 2^-10 and less than 12.  Each
+// group of either is then exact.
+#pragma once
+#include "ft_device.h"
+#include "ft_kernels.h"
+
+namespace ft {
+
+namespace {
+
+constexpr int XK = 128;                   // reduction elements per stage
+constexpr int XLR = 32;                   // low-rank columns per stage
+constexpr int kCuLdsBytes = 160 * 1024;
+
+template <int TM, int TN>
+struct MxGeom {
+  static constexpr int OFF_W = TM * XK;                 // weight tile, U or D chunk
+  static constexpr int OFF_S = OFF_W + TN * (XK / 2);   // scales of the X rows, 4 bytes each
+  static constexpr int SLOT = OFF_S + TM * 4;
+  static constexpr int XL = TM / 32, WL = TN / 64, LOADS = XL + WL + 1;   // per wave and stage
+  static constexpr int MT = TM / 64, NT = TN / 64;      // 32x32 tiles per wave
+  static constexpr int NS = TM == 64 ? 4 : 3;           // ring slots
+  static constexpr int STG = 4 * 32 * (64 * 4 + 16);    // the epilogue's staging rows (in the ring)
+};
+
+template <int V> struct IC8 { static constexpr int value = V; };
+template <int N, class F, int I = 0>
+__device__ __forceinline__ void static_for(F&& f) {
+  if constexpr (I < N) {
+    f(IC8<I>{});
+    static_for<N, F, I + 1>(static_cast<F&&>(f));
+  }
+}
+
+template <int SA, int SB>
+__device__ __forceinline__ v16f mfma_w4x8(v4i w, v8i x, v16f c, int sw, int sx) {
+  const v8i a = {w[0], w[1], w[2], w[3], 0, 0, 0, 0};
+  return __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(a, x, c, 4, 0, SA, sw, SB, sx);
+}
+
+// Bytes of LDS that hold the weight's scales: TN / 32 tiles by 4 per stage.
+__host__ __device__ inline int mx_slab(int tn, int nst) { return (tn / 32 * 4 * nst + 15) & ~15; }
+
+}  // namespace
+
+template <bool BWD, int TM, int TN, int ACT, bool F32>
+__global__ __launch_bounds__(256, TM == 256 ? 1 : 2) void k_gemm_mx8(
+    const uint8_t* __restrict__ X, const uint8_t* __restrict__ Xs, const uint8_t* __restrict__ Wq,
+    const uint8_t* __restrict__ Ws, int M, int N, int K, const float* __restrict__ P, int R,
+    const uint16_t* __restrict__ LR, const uint16_t* __restrict__ bias, uint16_t* z, const void* res, void* out,
+    int tiles_m, int tiles_n) {
+  using G = MxGeom<TM, TN>;
+  constexpr int MT = G::MT, NT = G::NT, NS = G::NS;
+  extern __shared__ __attribute__((aligned(16))) uint8_t mxlds[];
+
+  // Each XCD takes a contiguous range of tiles, eight tile-rows at a time, so
+  // that the workgroups sharing W columns share an L2.
+  const int T = tiles_m * tiles_n, per = (T + 7) >> 3;
+  const int t = (blockIdx.x & 7) * per + (blockIdx.x >> 3);
+  if (t >= T || (int)(blockIdx.x >> 3) >= per) return;   // the whole workgroup
+  int mt, nt;
+  {
+    constexpr int GM = 8;
+    const int g = t / (GM * tiles_n), first = g * GM, gm = min(GM, tiles_m - first), w = t - g * GM * tiles_n;
+    mt = first + w % gm;
+    nt = w / gm;
+  }
+  const int m0 = mt * TM, n0 = nt * TN;
+  const int NO = BWD ? K : N, KR = BWD ? N : K;
+  const int nrow = min(TM, M - m0), ncol = min(TN, NO - n0);
+  const int ldw = K >> 1, nwkb = K >> 5, nkb = KR >> 5;
+  const int tid = threadIdx.x, lane = tid & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int r32 = lane & 31, h = lane >> 5, g16 = lane >> 4, t16 = lane & 15;
+  const int wm = wave >> 1, wn = wave & 1;
+
+  // Buffers start at the tile: 32-bit offsets hold any number of rows.
+  const v4i rx = rsrc_words(X + (size_t)m0 * KR, (uint32_t)nrow * KR);
+  const v4i rw = BWD ? rsrc_words(Wq + (n0 >> 1), (uint32_t)N * ldw - (n0 >> 1))
+                     : rsrc_words(Wq + (size_t)n0 * ldw, (uint32_t)ncol * ldw);
+  const int nst = (KR + XK - 1) / XK, nlr = (R + XLR - 1) / XLR, total = nst + nlr;
+  const v4i rxs = rsrc_words(Xs + (size_t)m0 * 4, (uint32_t)(((size_t)(nst - 1) * M + nrow) * 4));
+  const v4i rp = rsrc_words(P + (R ? (size_t)m0 * R : 0), (uint32_t)nrow * R * 4);
+  const v4i rl = BWD ? rsrc_words(LR + (R ? (size_t)n0 * R : 0), (uint32_t)ncol * R * 2)
+                     : rsrc_words(LR, (uint32_t)NO * R * 2);
+  const uint32_t lds0 = lds_addr(mxlds);
+  const int off_slab = NS * G::SLOT;
+
+  // ---------------- per-lane load offsets within a whole stage
+  const int r8 = lane >> 3, c8 = (lane & 7) ^ r8;
+  uint32_t x_off[G::XL], w_off[G::WL];
+  int w_pos[G::WL];                       // forward: chunk of the stage's row; backward: row of the stage
+#pragma unroll
+  for (int v = 0; v < G::XL; v++) {
+    const int r = (wave * G::XL + v) * 8 + r8;
+    x_off[v] = r < nrow ? (uint32_t)r * KR + (c8 ^ (v & 1)) * 16 : kOobOffset;
+  }
+#pragma unroll
+  for (int v = 0; v < G::WL; v++) {
+    const int ins = wave * G::WL + v;
+    if constexpr (!BWD) {                 // 16 rows of 64 bytes
+      const int r = 16 * ins + (lane >> 2), c = (lane & 3) ^ swz64(r);
+      w_pos[v] = c;
+      w_off[v] = r < ncol ? (uint32_t)r * ldw + c * 16 : kOobOffset;
+    } else {                              // rows of TN / 2 bytes: the tile's columns
+      constexpr int CH = TN / 32;         // chunks a row
+      const int r = ins * (64 / CH) + lane / CH;
+      const int c = (lane % CH) ^ (CH == 8 ? (r >> 1) & 7 : swz64(r));
+      w_pos[v] = r;
+      w_off[v] = c * 32 < ncol ? (uint32_t)r * ldw + c * 16 : kOobOffset;
+    }
+  }
+  const int sseg = wave % (TM / 64);      // every wave loads scales (some the same ones): equal counts
+  const uint32_t s_off = sseg * 64 + lane < nrow ? (uint32_t)(sseg * 64 + lane) * 4 : kOobOffset;
+
+  // Load `i` of a whole stage u into the slot at `base`.
+  auto load_full = [&](auto ic, int u, uint32_t base) {
+    constexpr int i = decltype(ic)::value;
+    if constexpr (i < G::XL) {
+      dma16(rx, base + (wave * G::XL + i) * 1024, x_off[i], (uint32_t)u * XK);
+    } else if constexpr (i < G::XL + G::WL) {
+      constexpr int v = i - G::XL;
+      dma16(rw, base + G::OFF_W + (wave * G::WL + v) * 1024, w_off[v], BWD ? (uint32_t)u * XK * ldw : (uint32_t)u * (XK / 2));
+    } else {
+      dma4(rxs, base + G::OFF_S + sseg * 256, s_off, (uint32_t)u * M * 4);
+    }
+  };
+  // Load `i` of any stage: the reduction's last, partial one, a low-rank one, or none (zeros).
+  auto load_any = [&](auto ic, int u, uint32_t base) {
+    constexpr int i = decltype(ic)::value;
+    if (u < nst) {
+      if constexpr (i < G::XL) {
+        dma16(rx, base + (wave * G::XL + i) * 1024, u * XK + 16 * (c8 ^ (i & 1)) < KR ? x_off[i] : kOobOffset, (uint32_t)u * XK);
+      } else if constexpr (i < G::XL + G::WL) {
+        constexpr int v = i - G::XL;
+        const bool in = u * XK + (BWD ? w_pos[v] : 32 * w_pos[v]) < KR;
+        dma16(rw, base + G::OFF_W + (wave * G::WL + v) * 1024, in ? w_off[v] : kOobOffset,
+              BWD ? (uint32_t)u * XK * ldw : (uint32_t)u * (XK / 2));
+      } else {
+        dma4(rxs, base + G::OFF_S + sseg * 256, s_off, (uint32_t)u * M * 4);
+      }
+    } else {
+      const int q = u - nst, left = u < total ? R - q * XLR : 0;   // low-rank columns from this stage on
+      if constexpr (i < G::XL) {
+        const int r = (wave * G::XL + i) * 8 + r8, c = c8 ^ (i & 1);
+        dma16(rp, base + (wave * G::XL + i) * 1024, 4 * c < left && r < nrow ? (uint32_t)r * R * 4 + c * 16 : kOobOffset,
+              u < total ? (uint32_t)q * 128 : 0u);
+      } else if constexpr (i < G::XL + G::WL) {
+        const int ins = wave * G::WL + i - G::XL;
+        uint32_t off = kOobOffset, so = 0;
+        if constexpr (!BWD) {             // [32 j][TN n]
+          constexpr int CH = TN / 8;
+          const int j = ins * (64 / CH) + lane / CH, c = (lane % CH) ^ (2 * (j & 3));
+          if (j < left && c * 8 < ncol) off = (uint32_t)j * NO * 2 + (uint32_t)(n0 + c * 8) * 2;
+          so = u < total ? (uint32_t)q * XLR * NO * 2 : 0u;
+        } else {                          // [TN k][32 j]
+          const int k = 16 * ins + (lane >> 2), c = (lane & 3) ^ swz64(k);
+          if (k < ncol && 8 * c < left) off = (uint32_t)k * R * 2 + c * 16;
+          so = u < total ? (uint32_t)q * 64 : 0u;
+        }
+        dma16(rl, base + G::OFF_W + ins * 1024, off, so);
+      } else {
+        dma4(rxs, base + G::OFF_S + sseg * 256, kOobOffset, 0);
+      }
+    }
+  };
+
+  // ---------------- weight scales into LDS, the first stages' loads
+  // forward [TN / 32 tiles][4 nst blocks], backward [4 nst blocks][TN / 32 tiles]
+  {
+    constexpr int TB = TN / 32;
+    if ((nwkb & 3) == 0) {
+      const int dw = TB * nst;                           // dwords
+      for (int i = tid; i < dw; i += 256) {
+        uint32_t d = 0;
+        if constexpr (!BWD) {
+          const int j = i / nst, b = 4 * (i - j * nst), nb = (n0 >> 5) + j;
+          if (nb < (N >> 5) && b < nwkb) d = *(const uint32_t*)(Ws + (size_t)nb * nwkb + b);
+        } else {
+          const int b = i / (TB / 4), kb = (n0 >> 5) + 4 * (i % (TB / 4));
+          if (b < nkb && kb < nwkb) d = *(const uint32_t*)(Ws + (size_t)b * nwkb + kb);
+        }
+        *(uint32_t*)(mxlds + off_slab + 4 * i) = d;
+      }
+    } else {                                             // rows that are not 4-byte aligned
+      for (int i = tid; i < TB * 4 * nst; i += 256) {
+        const int j = BWD ? i % TB : i / (4 * nst), b = BWD ? i / TB : i - j * 4 * nst;
+        const int nb = (n0 >> 5) + j;
+        const bool in = b < nkb && nb < (NO >> 5);
+        mxlds[off_slab + i] = in ? Ws[BWD ? (size_t)b * nwkb + nb : (size_t)nb * nwkb + b] : (uint8_t)0;
+      }
+    }
+  }
+#pragma unroll 1
+  for (int u = 0; u < NS; u++) static_for<G::LOADS>([&](auto ic) { load_any(ic, u, lds0 + (uint32_t)u * G::SLOT); });
+
+  // accumulators start at the bias of their columns
+  v16f acc[MT][NT];
+  {
+    const __amdgpu_buffer_rsrc_t rb = make_rsrc(bias, !BWD && bias ? (uint32_t)N * 2 : 0u);
+#pragma unroll
+    for (int j = 0; j < NT; j++)
+#pragma unroll
+      for (int q = 0; q < 4; q++) {
+        v2i bb = {0, 0};
+        if constexpr (!BWD)
+          bb = __builtin_bit_cast(v2i, __builtin_amdgcn_raw_buffer_load_b64(rb, (n0 + wn * (TN / 2) + 32 * j + 8 * q + 4 * h) * 2, 0, 0));
+        const float b4[4] = {bf16_to_f32((uint32_t)bb[0] & 0xFFFFu), bf16_to_f32((uint32_t)bb[0] >> 16),
+                             bf16_to_f32((uint32_t)bb[1] & 0xFFFFu), bf16_to_f32((uint32_t)bb[1] >> 16)};
+#pragma unroll
+        for (int i = 0; i < MT; i++)
+#pragma unroll
+          for (int e = 0; e < 4; e++) acc[i][j][4 * q + e] = b4[e];
+      }
+  }
+
+  // ---------------- fragment reads, one LDS read (two for the backward's weight) an op
+  const int sw_r = swz128(r32), sw_w = swz64(r32), sw_t = swz64(t16), sw_t8 = (t16 >> 1) & 7;
+  struct Frags { v4i x[MT][2], w[NT]; };
+  struct Scales { uint32_t x[MT], w[BWD ? 2 : NT]; };
+  auto read_x = [&](auto oc, const uint8_t* base, int kk, Frags& f) {
+    constexpr int i = decltype(oc)::value >> 1, e = decltype(oc)::value & 1;
+    f.x[i][e] = *(const v4i*)(base + (wm * (TM / 2) + i * 32 + r32) * XK + (((4 * kk + 2 * e + h) ^ sw_r) << 4));
+  };
+  auto read_w = [&](auto oc, const uint8_t* base, int kk, Frags& f) {
+    constexpr int j = decltype(oc)::value;
+    if constexpr (!BWD) {
+      f.w[j] = *(const v4i*)(base + G::OFF_W + (wn * (TN / 2) + j * 32 + r32) * 64 + (((2 * kk + h) ^ sw_w) << 4));
+    } else {
+      const int c = (wn * NT + j) ^ (TN == 256 ? sw_t8 : sw_t);
+      const uint8_t* p = base + G::OFF_W + (kk * 64 + 32 * h + t16) * (TN / 2) + (c << 4) + 8 * (g16 & 1);
+      const v2i lo = lds_read_tr4((const FT_LDS void*)p), hi = lds_read_tr4((const FT_LDS void*)(p + 16 * (TN / 2)));
+      f.w[j] = v4i{lo[0], lo[1], hi[0], hi[1]};
+    }
+  };
+  constexpr int XOPS = 2 * MT, FOPS = XOPS + NT, SOPS = FOPS + MT + (BWD ? 2 : NT);
+  // in the last stage, bytes past the reduction's end become neutral
+  uint32_t keep_last = 0;
+#pragma unroll
+  for (int b = 0; b < 4; b++)
+    if (4 * (nst - 1) + b < nkb) keep_last |= 0xFFu << (8 * b);
+  // Scale words of stage s: X and forward W byte 2 kk = block 2 kk + h; backward W[kk] byte j = tile j.
+  auto read_s = [&](auto oc, const uint8_t* base, int s, Scales& f) {
+    constexpr int o = decltype(oc)::value;
+    if constexpr (o < MT) {
+      const uint32_t keep = s == nst - 1 ? keep_last : 0xFFFFFFFFu;
+      const uint32_t d = *(const uint32_t*)(base + G::OFF_S + (wm * (TM / 2) + o * 32 + r32) * 4);
+      f.x[o] = ((d & keep) | (0x7F7F7F7Fu & ~keep)) >> (8 * h);
+    } else if constexpr (!BWD) {
+      f.w[o - MT] = *(const uint32_t*)(mxlds + off_slab + ((wn * NT + o - MT) * nst + s) * 4) >> (8 * h);
+    } else {
+      const uint8_t* p = mxlds + off_slab + (4 * s + 2 * (o - MT) + h) * (TN / 32) + wn * NT;
+      if constexpr (NT == 4) f.w[o - MT] = *(const uint32_t*)p;
+      else f.w[o - MT] = *(const uint16_t*)p;
+    }
+  };
+  auto read_op = [&](auto oc, const uint8_t* base, int kk, int s, Frags& f, Scales& sc) {
+    constexpr int o = decltype(oc)::value;
+    if constexpr (o < XOPS) read_x(oc, base, kk, f);
+    else if constexpr (o < FOPS) read_w(IC8<o - XOPS>{}, base, kk, f);
+    else read_s(IC8<o - FOPS>{}, base, s, sc);
+  };
+  v8i xb, xl;                             // row tile i of X: all of it, or (F32) its parts from 2 up and below
+  auto mfma = [&](auto kc, auto tc, const Frags& f, const Scales& sc) {
+    constexpr int KK = decltype(kc)::value, i = decltype(tc)::value / NT, j = decltype(tc)::value % NT;
+    constexpr int SA = BWD ? j : 2 * KK, SB = 2 * KK;
+    const int sw = (int)sc.w[BWD ? KK : j], sx = (int)sc.x[i];
+    if constexpr (j == 0) {
+      xb = v8i{f.x[i][0][0], f.x[i][0][1], f.x[i][0][2], f.x[i][0][3], f.x[i][1][0], f.x[i][1][1], f.x[i][1][2], f.x[i][1][3]};
+      if constexpr (F32) split_e4m3(xb, xl);
+    }
+    acc[i][j] = mfma_w4x8<SA, SB>(f.w[j], xb, acc[i][j], sw, sx);
+    if constexpr (F32) acc[i][j] = mfma_w4x8<SA, SB>(f.w[j], xl, acc[i][j], sw, sx);
+  };
+
+  // Stage s + 1 is published in the middle of stage s: by then this wave holds
+  // all of stage s in registers, so its slot takes stage s + NS.
+  auto publish = [&](auto behind) {       // that many stages may stay in flight
+    wait_vm<G::LOADS * decltype(behind)::value>();
+    __builtin_amdgcn_s_waitcnt(0xc07f);   // this wave's LDS reads (and writes) are done
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");        // no LDS read moves above the barrier
+  };
+  publish(IC8<NS - 1>{});
+  Frags f0, f1;
+  Scales sc;
+  static_for<SOPS>([&](auto oc) { read_op(oc, mxlds, 0, 0, f0, sc); });
+  int slot = 0;
+  constexpr int MF = MT * NT;
+  auto body = [&](int s, auto fullc) {
+    const int next = slot + 1 == NS ? 0 : slot + 1;
+    const uint8_t* here = mxlds + slot * G::SLOT;
+    const uint8_t* there = mxlds + next * G::SLOT;
+    const uint32_t dst = lds0 + (uint32_t)slot * G::SLOT;
+    Scales scn;
+    static_for<MF>([&](auto tc) {
+      constexpr int t = decltype(tc)::value;
+      mfma(IC8<0>{}, tc, f0, sc);
+      static_for<(t + 1) * FOPS / MF - t * FOPS / MF>([&](auto e) {
+        read_op(IC8<t * FOPS / MF + decltype(e)::value>{}, here, 1, s, f1, scn);
+      });
+      __builtin_amdgcn_sched_barrier(0);
+    });
+    publish(IC8<NS - 2>{});
+    const int sn = min(s + 1, nst - 1);   // unused when stage s + 1 is a low-rank one
+    static_for<MF>([&](auto tc) {
+      constexpr int t = decltype(tc)::value;
+      mfma(IC8<1>{}, tc, f1, sc);
+      static_for<(t + 1) * SOPS / MF - t * SOPS / MF>([&](auto e) {
+        read_op(IC8<t * SOPS / MF + decltype(e)::value>{}, there, 0, sn, f0, scn);
+      });
+      static_for<(t + 1) * G::LOADS / MF - t * G::LOADS / MF>([&](auto e) {
+        constexpr int i = t * G::LOADS / MF + decltype(e)::value;
+        if constexpr (decltype(fullc)::value != 0) load_full(IC8<i>{}, s + NS, dst);
+        else load_any(IC8<i>{}, s + NS, dst);
+      });
+      __builtin_amdgcn_sched_barrier(0);
+    });
+    sc = scn;
+    slot = next;
+  };
+  const int nfull = KR / XK;
+  int s = 0;
+#pragma unroll 1
+  for (; s + NS < nfull; s++) body(s, IC8<1>{});
+#pragma unroll 1
+  for (; s < nst; s++) body(s, IC8<0>{});
+
+  // ---------------- low-rank stages: 16 columns at a time, P in two bf16 terms (F32: three)
+  const int jj = t16 >> 2, qq = t16 & 3;
+  auto lr_half = [&](const uint8_t* base, int c) {
+    v8bf b[NT];
+#pragma unroll
+    for (int j = 0; j < NT; j++) {
+      if constexpr (!BWD) {
+        const int n = wn * (TN / 2) + j * 32 + 16 * (g16 & 1) + 4 * qq, row = 16 * c + 8 * h + jj;
+        const int ch = (n >> 3) ^ (2 * (row & 3));   // row + 4 has the same swizzle
+        const uint8_t* p = base + G::OFF_W + row * (TN * 2) + (ch << 4) + ((n >> 2) & 1) * 8;
+        b[j] = make_v8bf(lds_read_tr16((const FT_LDS void*)p), lds_read_tr16((const FT_LDS void*)(p + 4 * TN * 2)));
+      } else {
+        b[j] = __builtin_bit_cast(v8bf, *(const v4i*)(base + G::OFF_W + (wn * (TN / 2) + j * 32 + r32) * 64 + (((2 * c + h) ^ sw_w) << 4)));
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < MT; i++) {
+      v4f x[2];
+      v4i part[F32 ? 3 : 2];              // terms of P: 16 significant bits, or 24
+#pragma unroll
+      for (int e = 0; e < 2; e++)
+        x[e] = *(const v4f*)(base + (wm * (TM / 2) + i * 32 + r32) * 128 + (((4 * c + 2 * h + e) ^ sw_r) << 4));
+#pragma unroll
+      for (int e = 0; e < 4; e++) {
+        const float a = x[e >> 1][2 * (e & 1)], d = x[e >> 1][2 * (e & 1) + 1];
+        uint32_t hi, lo;
+        split_bf16x2(a, d, hi, lo);
+        part[0][e] = (int)hi;
+        part[1][e] = (int)lo;
+        if constexpr (F32) {
+          const v2f left = {a - __uint_as_float(hi << 16) - __uint_as_float(lo << 16),
+                            d - __uint_as_float(hi & 0xFFFF0000u) - __uint_as_float(lo & 0xFFFF0000u)};
+          part[2][e] = (int)__builtin_bit_cast(uint32_t, __builtin_convertvector(left, v2bf));
+        }
+      }
+#pragma unroll
+      for (int p = 0; p < (F32 ? 3 : 2); p++)
+#pragma unroll
+        for (int j = 0; j < NT; j++) acc[i][j] = mfma_bf16_32x32x16(b[j], __builtin_bit_cast(v8bf, part[p]), acc[i][j]);
+    }
+  };
+#pragma unroll 1
+  for (; s < total; s++) {
+    const uint8_t* base = mxlds + slot * G::SLOT;
+    lr_half(base, 0);
+    if (R - (s - nst) * XLR > 16) lr_half(base, 1);
+    publish(IC8<NS - 2>{});
+    static_for<G::LOADS>([&](auto ic) { load_any(ic, s + NS, lds0 + (uint32_t)slot * G::SLOT); });
+    slot = slot + 1 == NS ? 0 : slot + 1;
+  }
+  wait_vm<0>();   // zeros of stages past the end must not land in the epilogue's LDS
+  __syncthreads();
+
+  // ---------------- epilogue: 32 rows x 64 columns at a time through the wave's own LDS
+  // Eight lanes hold 64 columns of a row, eight each, so that every global
+  // access is a whole 128-byte line of a row (256 bytes in fp32).  Everything
+  // is fp32 until the one rounding of each output.
+  constexpr int SROW = 64 * 4 + 16;
+  uint8_t* stg = mxlds + wave * (32 * SROW);
+  constexpr int es = F32 ? 4 : 2;
+  const size_t tile0 = (size_t)m0 * NO + n0;
+  const uint32_t span = (uint32_t)(nrow - 1) * NO + ncol;   // elements from the tile's first to its last
+  const __amdgpu_buffer_rsrc_t ro = make_rsrc((uint8_t*)out + tile0 * es, span * es);
+  const __amdgpu_buffer_rsrc_t rr = make_rsrc(res ? (const uint8_t*)res + tile0 * es : nullptr, res ? span * es : 0u);
+  const __amdgpu_buffer_rsrc_t rz = make_rsrc(z ? z + tile0 : nullptr, z ? span * 2 : 0u);
+#pragma unroll
+  for (int i = 0; i < MT; i++)
+#pragma unroll
+    for (int jp = 0; jp < NT / 2; jp++) {
+      // element offset of this lane's eight columns in the tile, or none
+      uint32_t at[4];
+#pragma unroll
+      for (int it = 0; it < 4; it++) {
+        const int r = wm * (TM / 2) + 32 * i + it * 8 + (lane >> 3), c = wn * (TN / 2) + 64 * jp + (lane & 7) * 8;
+        at[it] = r < nrow && c < ncol ? (uint32_t)r * NO + c : kOobOffset;
+      }
+      v4i zv[4], rv[4][2];
+      if (BWD && ACT != ACT_NONE) {
+#pragma unroll
+        for (int it = 0; it < 4; it++)
+          zv[it] = __builtin_bit_cast(v4i, __builtin_amdgcn_raw_buffer_load_b128(rz, at[it] == kOobOffset ? kOobOffset : at[it] * 2, 0, 0));
+      }
+      if (res) {
+#pragma unroll
+        for (int it = 0; it < 4; it++) {
+          const uint32_t o = at[it] == kOobOffset ? kOobOffset : at[it] * es;
+          rv[it][0] = __builtin_bit_cast(v4i, __builtin_amdgcn_raw_buffer_load_b128(rr, o, 0, 0));
+          if (F32) rv[it][1] = __builtin_bit_cast(v4i, __builtin_amdgcn_raw_buffer_load_b128(rr, o, 16, 0));
+        }
+      }
+#pragma unroll
+      for (int jh = 0; jh < 2; jh++)
+#pragma unroll
+        for (int q = 0; q < 4; q++) {
+          const v16f& a = acc[i][2 * jp + jh];
+          *(v4f*)(stg + r32 * SROW + (32 * jh + 8 * q + 4 * h) * 4) = v4f{a[4 * q], a[4 * q + 1], a[4 * q + 2], a[4 * q + 3]};
+        }
+      __builtin_amdgcn_s_waitcnt(0xc07f);               // the wave reads back only its own rows
+#pragma unroll
+      for (int it = 0; it < 4; it++) {
+        const uint8_t* p = stg + (it * 8 + (lane >> 3)) * SROW + (lane & 7) * 32;
+        const v4f lo = *(const v4f*)p, hi = *(const v4f*)(p + 16);
+        float f[8] = {lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
+        const uint32_t o = at[it] == kOobOffset ? kOobOffset : at[it] * es;
+        if constexpr (!BWD) {
+          if (z) __builtin_amdgcn_raw_buffer_store_b128(pack_bf16x8(f), rz, at[it] == kOobOffset ? kOobOffset : at[it] * 2, 0, 0);
+#pragma unroll
+          for (int e = 0; e < 8; e++) f[e] = act_fn<ACT>(f[e]);
+        } else if constexpr (ACT != ACT_NONE) {
+          float zf[8];
+          unpack_bf16x8(zv[it], zf);
+#pragma unroll
+          for (int e = 0; e < 8; e++) f[e] *= act_grad<ACT>(zf[e]);
+        }
+        if (res) {
+          float rf[8];
+          if constexpr (F32) {
+#pragma unroll
+            for (int e = 0; e < 8; e++) rf[e] = __int_as_float(rv[it][e >> 2][e & 3]);
+          } else {
+            unpack_bf16x8(rv[it][0], rf);
+          }
+#pragma unroll
+          for (int e = 0; e < 8; e++) f[e] += rf[e];
+        }
+        if constexpr (F32) {
+          __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(v4i, v4f{f[0], f[1], f[2], f[3]}), ro, o, 0, 0);
+          __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(v4i, v4f{f[4], f[5], f[6], f[7]}), ro, o, 16, 0);
+        } else {
+          __builtin_amdgcn_raw_buffer_store_b128(pack_bf16x8(f), ro, o, 0, 0);
+        }
+      }
+      asm volatile("" ::: "memory");                    // the next pass's staging writes stay behind these reads
+    }
+}
+
+template <bool F32>
+hipError_t launch_gemm_mx8_t(bool bwd, int tm, const MxArgs& a, int act, hipStream_t st) {
+  const int NO = bwd ? a.K : a.N, nst = ((bwd ? a.N : a.K) + XK - 1) / XK;
+  const int tn = tm == 256 ? 256 : 128;
+  const int tiles_m = (a.M + tm - 1) / tm, tiles_n = (NO + tn - 1) / tn;
+  const unsigned grid = (unsigned)(((long)tiles_m * tiles_n + 7) / 8 * 8);
+#define FT_MX(BW, TM_, TN_, ACT_)                                                                                   \
+  do {                                                                                                              \
+    using G = MxGeom<TM_, TN_>;                                                                                     \
+    static_assert(G::NS * G::SLOT >= G::STG, "the epilogue's rows lie in the ring");                                \
+    k_gemm_mx8<BW, TM_, TN_, ACT_, F32><<<grid, 256, (size_t)G::NS * G::SLOT + mx_slab(TN_, nst), st>>>(            \
+        a.x, a.xs, a.wq, a.ws, a.M, a.N, a.K, a.P, a.R, a.lr, a.bias, a.z, a.res, a.out, tiles_m, tiles_n);         \
+  } while (0)
+#define FT_MX_ACT(BW, TM_, TN_)                                   \
+  do {                                                            \
+    if (act == ACT_GELU) FT_MX(BW, TM_, TN_, ACT_GELU);           \
+    else if (act == ACT_SILU) FT_MX(BW, TM_, TN_, ACT_SILU);      \
+    else if (act == ACT_RELU) FT_MX(BW, TM_, TN_, ACT_RELU);      \
+    else FT_MX(BW, TM_, TN_, ACT_NONE);                           \
+  } while (0)
+  if (tm == 256) { if (!bwd) FT_MX_ACT(false, 256, 256); else FT_MX_ACT(true, 256, 256); }
+  else if (tm == 128) { if (!bwd) FT_MX_ACT(false, 128, 128); else FT_MX_ACT(true, 128, 128); }
+  else { if (!bwd) FT_MX_ACT(false, 64, 128); else FT_MX_ACT(true, 64, 128); }
+#undef FT_MX_ACT
+#undef FT_MX
+  return hipGetLastError();
+}
+
+}  // namespace ft

@@ -63,6 +63,9 @@ __device__ __forceinline__ void swap_halves(uint32_t& a, uint32_t& b) {
 }  // namespace
 
 // MODE 1: proj is [cols, R]; MODE 2: proj is [R, cols].
+// QM_E4M3: MXFP8 instead of MXFP4 (codes [rows, cols], scales [cols / 128, rows,
+// 4]).  A lane pair holds 16 bytes of a block as two runs of 8; one swap makes
+// them one run of 16 per lane, two stores a step.
 template <int RT, int MODE, int QM, bool GELU>
 __global__ __launch_bounds__(256) void k_quant_proj(const uint16_t* __restrict__ src, int rows, int cols,
                                                     uint8_t* __restrict__ codes, uint8_t* __restrict__ scales,
@@ -84,7 +87,9 @@ __global__ __launch_bounds__(256) void k_quant_proj(const uint16_t* __restrict__
   // any row count.
   const v4i rx = rsrc_words(src + (size_t)row0 * cols, (uint32_t)nrow * cols * 2);
   const v4i rp = rsrc_words(proj, (uint32_t)R * cols * 2);
-  const __amdgpu_buffer_rsrc_t rc = make_rsrc(codes + (size_t)row0 * (cols >> 1), (uint32_t)nrow * (cols >> 1));
+  constexpr bool E4M3 = (QM & QM_E4M3) != 0;
+  const int ldc = E4M3 ? cols : cols >> 1;           // bytes of a row of codes
+  const __amdgpu_buffer_rsrc_t rc = make_rsrc(codes + (size_t)row0 * ldc, (uint32_t)nrow * ldc);
   const __amdgpu_buffer_rsrc_t rh = make_rsrc(GELU ? h_out + (size_t)row0 * cols : nullptr, GELU ? (uint32_t)nrow * cols * 2 : 0u);
 
   // Row load i brings rows 8 i + lane / 8 of the wave's 32; physical chunk
@@ -130,7 +135,7 @@ __global__ __launch_bounds__(256) void k_quant_proj(const uint16_t* __restrict__
     for (int e = 0; e < G::SETS; e++) acc[t][e] = v16f{};
   const int sw = swz128(r32);
   const int wrow = wave * 32 + r32;                // this lane's row within the workgroup
-  const uint32_t coff = wrow < nrow ? (uint32_t)wrow * (cols >> 1) + 16 * h : kOobOffset;
+  const uint32_t coff = wrow < nrow ? (uint32_t)wrow * ldc + 16 * h : kOobOffset;
   uint32_t sword = 0;                              // scale bytes of a pair of steps
   int slot = 0;
 
@@ -139,7 +144,7 @@ __global__ __launch_bounds__(256) void k_quant_proj(const uint16_t* __restrict__
     // Step s's loads have landed: all but those of the NS - 2 steps behind it
     // and, once NS - 1 steps have run, the stores of those steps (at least
     // STORES each), which were issued after them too.
-    constexpr int STORES = GELU ? 5 : 1;
+    constexpr int STORES = GELU ? 5 : E4M3 ? 2 : 1;
     if (s - s0 >= G::NS - 1) wait_vm<G::LOADS * (G::NS - 2) + STORES * (G::NS - 1)>();
     else wait_vm<G::LOADS * (G::NS - 2)>();
     static_assert(G::LOADS * (G::NS - 2) + STORES * (G::NS - 1) < 64, "vmcnt range");
@@ -166,7 +171,8 @@ __global__ __launch_bounds__(256) void k_quant_proj(const uint16_t* __restrict__
     v4i x[4];
 #pragma unroll
     for (int kk = 0; kk < 4; kk++) x[kk] = *(const v4i*)(xb + r32 * 128 + (((2 * kk + h) ^ sw) << 4));
-    uint32_t o[4], code[2];
+    uint32_t code[2];
+    uint32_t o[E4M3 ? 8 : 4];                        // codes of x[kk] (FP4: one dword each; FP8: two)
 #pragma unroll
     for (int b = 0; b < 2; b++) {
       v2u16 p[8];
@@ -178,33 +184,60 @@ __global__ __launch_bounds__(256) void k_quant_proj(const uint16_t* __restrict__
         for (int e = 0; e < n; e++) p[e] = __builtin_elementwise_max(p[e], p[e + n]);
       uint32_t m = max((uint32_t)p[0][0], (uint32_t)p[0][1]), other = m;
       swap_halves(m, other);
-      code[b] = e8m0_of<QM>(max(m, other));
+      m = max(m, other);
+      code[b] = E4M3 ? e8m0_e4m3_from_bf16(m) : e8m0_of<QM>(m);
       const float sc = e8m0_to_f32(code[b]);
 #pragma unroll
       for (int u = 0; u < 2; u++) {
         const v4i w = x[2 * b + u];
-        uint32_t q = 0;
-        q = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(q, __builtin_bit_cast(v2bf, (int)w[0]), sc, 0);
-        q = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(q, __builtin_bit_cast(v2bf, (int)w[1]), sc, 1);
-        q = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(q, __builtin_bit_cast(v2bf, (int)w[2]), sc, 2);
-        q = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(q, __builtin_bit_cast(v2bf, (int)w[3]), sc, 3);
-        o[2 * b + u] = q;
+        if constexpr (E4M3) {
+#pragma unroll
+          for (int e = 0; e < 2; e++) {
+            v2s q = {0, 0};
+            q = __builtin_amdgcn_cvt_scalef32_pk_fp8_bf16(q, __builtin_bit_cast(v2bf, (int)w[2 * e]), sc, false);
+            q = __builtin_amdgcn_cvt_scalef32_pk_fp8_bf16(q, __builtin_bit_cast(v2bf, (int)w[2 * e + 1]), sc, true);
+            o[4 * b + 2 * u + e] = __builtin_bit_cast(uint32_t, q);
+          }
+        } else {
+          uint32_t q = 0;
+          q = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(q, __builtin_bit_cast(v2bf, (int)w[0]), sc, 0);
+          q = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(q, __builtin_bit_cast(v2bf, (int)w[1]), sc, 1);
+          q = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(q, __builtin_bit_cast(v2bf, (int)w[2]), sc, 2);
+          q = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(q, __builtin_bit_cast(v2bf, (int)w[3]), sc, 3);
+          o[2 * b + u] = q;
+        }
       }
     }
-    // codes of chunks h, 2 + h, 4 + h, 6 + h -> the lower half-wave's 0..3, the upper's 4..7
-    swap_halves(o[0], o[2]);
-    swap_halves(o[1], o[3]);
-    __builtin_amdgcn_raw_buffer_store_b128(v4i{(int)o[0], (int)o[2], (int)o[1], (int)o[3]}, rc,
-                                           64 * s + 32 * h < cols ? coff : kOobOffset, s * 32, 0);
+    if constexpr (E4M3) {
+      // bytes 16 kk + 8 h of a block's kk = 0, 1 -> the lower half-wave's first 16, the upper's last 16
+#pragma unroll
+      for (int b = 0; b < 2; b++) {
+        swap_halves(o[4 * b], o[4 * b + 2]);
+        swap_halves(o[4 * b + 1], o[4 * b + 3]);
+        __builtin_amdgcn_raw_buffer_store_b128(v4i{(int)o[4 * b], (int)o[4 * b + 1], (int)o[4 * b + 2], (int)o[4 * b + 3]},
+                                               rc, 64 * s + 32 * b < cols ? coff : kOobOffset, s * 64 + 32 * b, 0);
+      }
+      if (64 * s + 32 >= cols) code[1] = 127u;       // blocks past the row's end: 1
+    } else {
+      // codes of chunks h, 2 + h, 4 + h, 6 + h -> the lower half-wave's 0..3, the upper's 4..7
+      swap_halves(o[0], o[2]);
+      swap_halves(o[1], o[3]);
+      __builtin_amdgcn_raw_buffer_store_b128(v4i{(int)o[0], (int)o[2], (int)o[1], (int)o[3]}, rc,
+                                             64 * s + 32 * h < cols ? coff : kOobOffset, s * 32, 0);
+    }
     // scale bytes: a pair of steps (runs begin at even steps) is one dword of the row
     const uint32_t two = code[0] | (code[1] << 8);
-    sword = (s & 1) ? sword | (two << 16) : two;
+    sword = (s & 1) ? (sword & 0xFFFFu) | (two << 16) : two | 0x7F7F0000u;
     if (((s & 1) || s + 1 == s1) && h == 0 && wrow < nrow) {
-      uint8_t* d = scales + (size_t)(row0 + wrow) * nbc + 2 * (s & ~1);
-      const int n = min(4, nbc - 2 * (s & ~1));
-      if ((nbc & 3) == 0 && n == 4) *(uint32_t*)d = sword;
-      else
-        for (int b = 0; b < n; b++) d[b] = (uint8_t)(sword >> (8 * b));
+      if constexpr (E4M3) {
+        *(uint32_t*)(scales + ((size_t)(s >> 1) * rows + row0 + wrow) * 4) = sword;
+      } else {
+        uint8_t* d = scales + (size_t)(row0 + wrow) * nbc + 2 * (s & ~1);
+        const int n = min(4, nbc - 2 * (s & ~1));
+        if ((nbc & 3) == 0 && n == 4) *(uint32_t*)d = sword;
+        else
+          for (int b = 0; b < n; b++) d[b] = (uint8_t)(sword >> (8 * b));
+      }
     }
 #pragma unroll
     for (int kk = 0; kk < 4; kk++)
@@ -303,14 +336,29 @@ static hipError_t launch_qp(const uint16_t* src, int rows, int cols, uint8_t* co
 }
 
 hipError_t launch_quant_proj(const uint16_t* src, int rows, int cols, uint8_t* codes, uint8_t* scales,
-                             const uint16_t* proj, int R, int layout, bool no_clip, float* proj_out, float* ws,
+                             const uint16_t* proj, int R, int layout, int qm, float* proj_out, float* ws,
                              int max_groups, int max_chain, uint16_t* gelu_out, hipStream_t st) {
 #define FT_QPL(QM_, GELU_, LAYOUT_) \
   launch_qp<QM_, GELU_>(src, rows, cols, codes, scales, proj, R, LAYOUT_, proj_out, ws, max_groups, max_chain, gelu_out, st)
   if (gelu_out) return FT_QPL(0, true, 0);
-  if (no_clip) return FT_QPL(QM_NOCLIP, false, layout);
+  if (qm & QM_E4M3) return FT_QPL(QM_E4M3, false, layout);
+  if (qm & QM_NOCLIP) return FT_QPL(QM_NOCLIP, false, layout);
   return FT_QPL(0, false, layout);
 #undef FT_QPL
+}
+
+// MXFP8: at most as many partials as the chunked MXFP4 kernel's workspace would hold.
+size_t quant8_proj_workspace(int rows, int cols, int R, int layout) {
+  int groups, chain;
+  quant_rows_chain(rows, cols, R, layout, groups, chain);
+  return groups > 1 ? (size_t)groups * rows * R * sizeof(float) : 0;
+}
+
+hipError_t launch_quant8_proj(const uint16_t* src, int rows, int cols, uint8_t* codes, uint8_t* scales,
+                              const uint16_t* proj, int R, int layout, float* proj_out, float* ws, hipStream_t st) {
+  int groups, chain;
+  quant_rows_chain(rows, cols, R, layout, groups, chain);
+  return launch_quant_proj(src, rows, cols, codes, scales, proj, R, layout, QM_E4M3, proj_out, ws, groups, chain, nullptr, st);
 }
 
 }  // namespace ft

@@ -51,13 +51,6 @@ struct QuantLds {
 
 typedef unsigned short v2u16 __attribute__((ext_vector_type(2)));
 
-// max over the 4 lanes of each aligned quad
-__device__ __forceinline__ uint32_t quad_max(uint32_t m) {
-  m = max(m, (uint32_t)__builtin_amdgcn_mov_dpp((int)m, 0xB1, 0xF, 0xF, true));  // quad_perm [1,0,3,2]
-  m = max(m, (uint32_t)__builtin_amdgcn_mov_dpp((int)m, 0x4E, 0xF, 0xF, true));  // quad_perm [2,3,0,1]
-  return m;
-}
-
 // One 64-column step of a wave's 8*NQ rows (NQ groups of 8 rows): block
 // scales and codes, the scale bytes staged in the wave's LDS rows, and (XT)
 // the step's bf16 values in the wave's projection tile.  EDGE: rows past
@@ -671,7 +664,7 @@ static hipError_t launch_quant_rows_qm(const uint16_t* src, int rows, int cols, 
     if (quant_proj_supported(rows, cols, R)) {
       int groups, chain;
       quant_rows_chain(rows, cols, R, layout, groups, chain);
-      return launch_quant_proj(src, rows, cols, codes, scales, proj, R, layout, (QM & QM_NOCLIP) != 0, proj_out, ws,
+      return launch_quant_proj(src, rows, cols, codes, scales, proj, R, layout, QM & QM_NOCLIP, proj_out, ws,
                                groups, chain, nullptr, st);
     }
   }
