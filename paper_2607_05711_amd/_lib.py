@@ -521,28 +521,53 @@ def ft_linear_bwd_input_nvfp4(gq, gs, gt, wq, ws, wt, K):
 F8 = torch.float8_e4m3fn
 
 
+_get_device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
+_Tensor = torch.Tensor
+
+
 def _launch(f, dev, *args):
-    """f on this device's current stream."""
-    if torch.cuda.current_device() == dev.index:
-        _check(f(*args, _stream(dev)))
+    """f on the current stream of device number dev."""
+    if _get_device() == dev:
+        status = f(*args, _raw_stream(dev) if _raw_stream is not None else torch.cuda.current_stream(dev).cuda_stream)
     else:
         with torch.cuda.device(dev):
-            _check(f(*args, _stream(dev)))
+            status = f(*args, torch.cuda.current_stream(dev).cuda_stream)
+    if status != FT_OK:
+        _check(status)
 
 
-def _like(t, name, shape, dtype, dev):
-    """The caller's output (checked) or a new one."""
+def _gpu(t, name, dtype, ndim):
+    """The number of the device that holds this tensor (checked)."""
+    # (host time is most of a small call's: one pass here and in _fits, what fails it is named by _need)
+    if isinstance(t, _Tensor) and t.dtype is dtype and t.is_contiguous() and t.dim() == ndim:
+        dev = t.get_device()
+        if dev >= 0:
+            return dev
+    return _need(t, name, dtype, ndim=ndim).get_device()
+
+
+def _fits(t, name, shape, dtype, dev):
+    """Checks a tensor and gives its address."""
+    if isinstance(t, _Tensor) and t.dtype is dtype and t.get_device() == dev and t.is_contiguous() and t.shape == shape:
+        return t.data_ptr()
+    _need(t, name, dtype, torch.device("cuda", dev))
+    raise ValueError("%s must be %s, got %s" % (name, tuple(shape), tuple(t.shape)))
+
+
+def _out(t, name, shape, dtype, dev):
+    """The caller's output (checked) or a new one, and its address."""
     if t is None:
-        return torch.empty(shape, dtype=dtype, device=dev)
-    _need(t, name, dtype, dev)
-    if t.shape != shape:
-        raise ValueError("%s must be %s, got %s" % (name, tuple(shape), tuple(t.shape)))
-    return t
+        t = torch.empty(shape, dtype=dtype, device=dev)
+        return t, t.data_ptr()
+    return t, _fits(t, name, shape, dtype, dev)
 
 
-def _opt(t, name, shape, dtype, dev):
-    """An optional input (checked)."""
-    return None if t is None else _like(t, name, shape, dtype, dev)
+def _space(nbytes, dev, workspace):
+    """The caller's workspace or a new one: (tensor, address, bytes)."""
+    if nbytes == 0 and workspace is None:
+        return None, None, 0
+    workspace = _workspace(nbytes, dev, workspace)
+    return workspace, workspace.data_ptr(), _nbytes(workspace)
 
 
 def scales8_shape(rows, cols):
@@ -561,26 +586,25 @@ def ft_rmsnorm_quantize8(x, w, residual=None, eps=1e-6, h=None, y=None, codes=No
     fp32 [rows] or None.  y, codes and rstd are made where an output is passed or
     asked for.
     """
-    L = load()
-    _need(x, "x", torch.bfloat16, ndim=2)
-    dev, (rows, cols) = x.device, x.shape
-    _need(w, "w", torch.bfloat16, dev, ndim=1)
-    if w.shape[0] != cols:
-        raise ValueError("w must be [%d]" % cols)
+    BF = torch.bfloat16
+    dev = _gpu(x, "x", BF, 2)
+    shape = x.shape
+    rows, cols = shape
+    pw = _fits(w, "w", (cols,), BF, dev)
+    pr = ph = py = pc = ps = pd = None
     if residual is not None:
-        _like(residual, "residual", x.shape, torch.bfloat16, dev)
-        h = _like(h, "h", x.shape, torch.bfloat16, dev)
+        pr = _fits(residual, "residual", shape, BF, dev)
+        h, ph = _out(h, "h", shape, BF, dev)
     elif h is not None:
         raise ValueError("h goes with a residual")
     if y is not None or want_y:
-        y = _like(y, "y", x.shape, torch.bfloat16, dev)
+        y, py = _out(y, "y", shape, BF, dev)
     if codes is not None or scales is not None or want_codes:
-        codes = _like(codes, "codes", x.shape, F8, dev)
-        scales = _like(scales, "scales", scales8_shape(rows, cols), torch.uint8, dev)
+        codes, pc = _out(codes, "codes", shape, F8, dev)
+        scales, ps = _out(scales, "scales", scales8_shape(rows, cols), torch.uint8, dev)
     if rstd is not None or want_rstd:
-        rstd = _like(rstd, "rstd", (rows,), torch.float32, dev)
-    _launch(L.ft_rmsnorm_quantize8, dev, _ptr(x), _ptr(residual), _ptr(w), rows, cols, eps, _ptr(h), _ptr(y), _ptr(codes),
-            _ptr(scales), _ptr(rstd))
+        rstd, pd = _out(rstd, "rstd", (rows,), torch.float32, dev)
+    _launch(load().ft_rmsnorm_quantize8, dev, x.data_ptr(), pr, pw, rows, cols, eps, ph, py, pc, ps, pd)
     return (x if residual is None else h), y, codes, scales, rstd
 
 
@@ -588,19 +612,21 @@ def ft_rmsnorm_bwd(dy, h, w, rstd, dh=None, dx=None, dw=None, want_dw=True, work
     """Gradients of ft_rmsnorm_quantize8's y: (dx bf16 [rows, cols], of x and of
     the residual alike, dw fp32 [cols] or None).  dh: the gradient that reaches h
     on the residual stream; dx may be dy or dh."""
-    L = load()
-    _need(dy, "dy", torch.bfloat16, ndim=2)
-    dev, (rows, cols) = dy.device, dy.shape
-    _like(h, "h", dy.shape, torch.bfloat16, dev)
-    _like(w, "w", (cols,), torch.bfloat16, dev)
-    _like(rstd, "rstd", (rows,), torch.float32, dev)
-    _opt(dh, "dh", dy.shape, torch.bfloat16, dev)
-    dx = _like(dx, "dx", dy.shape, torch.bfloat16, dev)
+    BF, L = torch.bfloat16, load()
+    dev = _gpu(dy, "dy", BF, 2)
+    shape = dy.shape
+    rows, cols = shape
+    ph = _fits(h, "h", shape, BF, dev)
+    pw = _fits(w, "w", (cols,), BF, dev)
+    pr = _fits(rstd, "rstd", (rows,), torch.float32, dev)
+    pd = None if dh is None else _fits(dh, "dh", shape, BF, dev)
+    dx, px = _out(dx, "dx", shape, BF, dev)
+    pg = ps = None
+    n = 0
     if dw is not None or want_dw:
-        dw = _like(dw, "dw", (cols,), torch.float32, dev)
-        workspace = _workspace(L.ft_rmsnorm_bwd_workspace_size(rows, cols), dev, workspace)
-    _launch(L.ft_rmsnorm_bwd, dev, _ptr(dy), _ptr(dh), _ptr(h), _ptr(w), _ptr(rstd), rows, cols, _ptr(dx), _ptr(dw),
-            _ptr(workspace), _nbytes(workspace))
+        dw, pg = _out(dw, "dw", (cols,), torch.float32, dev)
+        workspace, ps, n = _space(L.ft_rmsnorm_bwd_workspace_size(rows, cols), dev, workspace)
+    _launch(L.ft_rmsnorm_bwd, dev, dy.data_ptr(), pd, ph, pw, pr, rows, cols, px, pg, ps, n)
     return dx, dw
 
 
@@ -617,26 +643,29 @@ def ft_quantize8(src, z=None, act=FT_ACT_NONE, proj=None, proj_layout=FT_PROJ_CO
     quantized is src * act'(z), which v holds in bf16 (None without want_v; v may
     be src).
     """
-    L = load()
-    _need(src, "src", torch.bfloat16, ndim=2)
-    dev, (rows, cols) = src.device, src.shape
-    codes = _like(codes, "codes", src.shape, F8, dev)
-    scales = _like(scales, "scales", scales8_shape(rows, cols), torch.uint8, dev)
-    _opt(z, "z", src.shape, torch.bfloat16, dev)
-    if z is not None and (v is not None or want_v):
-        v = _like(v, "v", src.shape, torch.bfloat16, dev)
-    R = 0
+    BF, L = torch.bfloat16, load()
+    dev = _gpu(src, "src", BF, 2)
+    shape = src.shape
+    rows, cols = shape
+    codes, pc = _out(codes, "codes", shape, F8, dev)
+    scales, ps = _out(scales, "scales", scales8_shape(rows, cols), torch.uint8, dev)
+    pz = pv = pp = po = pws = None
+    R = n = 0
+    if z is not None:
+        pz = _fits(z, "z", shape, BF, dev)
+        if v is not None or want_v:
+            v, pv = _out(v, "v", shape, BF, dev)
+    elif v is not None:
+        raise ValueError("v goes with z")
     if proj is not None:
-        _need(proj, "proj", torch.bfloat16, dev, ndim=2)
-        R, other = proj.shape if proj_layout == FT_PROJ_R_BY_COLS else proj.shape[::-1]
-        if other != cols:
-            raise ValueError("proj shape %s does not match cols %d" % (tuple(proj.shape), cols))
-        proj_out = _like(proj_out, "proj_out", (rows, R), torch.float32, dev)
-        workspace = _workspace(L.ft_quantize8_workspace_size(rows, cols, R, proj_layout), dev, workspace)
+        _need(proj, "proj", BF, ndim=2)
+        R = proj.shape[0 if proj_layout == FT_PROJ_R_BY_COLS else 1]
+        pp = _fits(proj, "proj", (R, cols) if proj_layout == FT_PROJ_R_BY_COLS else (cols, R), BF, dev)
+        proj_out, po = _out(proj_out, "proj_out", (rows, R), torch.float32, dev)
+        workspace, pws, n = _space(L.ft_quantize8_workspace_size(rows, cols, R, proj_layout), dev, workspace)
     else:
         proj_out = None
-    _launch(L.ft_quantize8, dev, _ptr(src), _ptr(z), act, rows, cols, _ptr(v), _ptr(codes), _ptr(scales), _ptr(proj), R,
-            proj_layout, _ptr(proj_out), _ptr(workspace), _nbytes(workspace))
+    _launch(L.ft_quantize8, dev, src.data_ptr(), pz, act, rows, cols, pv, pc, ps, pp, R, proj_layout, po, pws, n)
     return codes, scales, proj_out, v
 
 
@@ -644,25 +673,35 @@ def ft_quantize8_workspace_size(rows, cols, R=0, proj_layout=FT_PROJ_COLS_BY_R):
     return int(load().ft_quantize8_workspace_size(rows, cols, R, proj_layout))
 
 
-def _linear8_operands(q, s, wq, ws, reduce_rows):
-    """(device, M, N, K) of an 8-bit product; reduce_rows: over the weight's rows N (the backward)."""
-    _need(q, "codes", F8, ndim=2)
-    dev = q.device
-    _need(wq, "wq", torch.uint8, dev, ndim=2)
-    _need(ws, "ws", torch.uint8, dev)
-    M, N, K = q.shape[0], wq.shape[0], 2 * wq.shape[1]
-    if q.shape[1] != (N if reduce_rows else K) or ws.numel() * 1024 != N * K:
+def _linear8_operands(q, s, wq, ws, axis):
+    """(device, M, N, K, addresses of codes, scales and the weight's) of an 8-bit product over the weight's axis."""
+    dev = _gpu(q, "codes", F8, 2)
+    M, KR = q.shape
+    if _gpu(wq, "wq", torch.uint8, 2) != dev or _need(ws, "ws", torch.uint8).get_device() != dev:
+        raise ValueError("the weight is on another device than the codes")
+    N, K = wq.shape
+    K *= 2
+    if KR != (K if axis else N) or ws.numel() * 1024 != N * K:
         raise ValueError("operand shapes do not match: codes %s, wq %s, ws %s" % (tuple(q.shape), tuple(wq.shape),
                                                                                tuple(ws.shape)))
-    _like(s, "scales", scales8_shape(M, q.shape[1]), torch.uint8, dev)
-    return dev, M, N, K
+    return dev, M, N, K, q.data_ptr(), _fits(s, "scales", scales8_shape(M, KR), torch.uint8, dev), wq.data_ptr(), ws.data_ptr()
+
+
+def _low_rank(P, F, names, shape, dev):
+    """(R, addresses) of the low-rank term's factors; shape: F's for a width R."""
+    if P is None and F is None:
+        return 0, None, None
+    _need(P, names[0], torch.float32, ndim=2)
+    R = P.shape[1]
+    M, fshape = shape(R)
+    return R, _fits(P, names[0], (M, R), torch.float32, dev), _fits(F, names[1], fshape, torch.bfloat16, dev)
 
 
 def _output8(out, name, shape, out_dtype, dev):
-    dt = out_dtype if out is None else out.dtype
-    if dt not in (torch.bfloat16, torch.float32):
+    dt = out_dtype if out is None else getattr(out, "dtype", None)
+    if dt is not torch.bfloat16 and dt is not torch.float32:
         raise ValueError("%s must be bf16 or fp32" % name)
-    return _like(out, name, shape, dt, dev)
+    return (dt,) + _out(out, name, shape, dt, dev)
 
 
 def ft_linear8_fwd(xq, xs, wq, ws, P=None, U=None, bias=None, act=FT_ACT_NONE, residual=None, out_dtype=torch.bfloat16,
@@ -671,22 +710,17 @@ def ft_linear8_fwd(xq, xs, wq, ws, P=None, U=None, bias=None, act=FT_ACT_NONE, r
     activations (xq float8_e4m3fn [M, K], xs uint8 [ceil(K / 128), M, 4]).
     residual has y's type and may be y.  Returns y, or (y, z) with z, act's input
     in bf16, where z is passed or asked for."""
-    L = load()
-    dev, M, N, K = _linear8_operands(xq, xs, wq, ws, False)
-    R = 0
-    if P is not None or U is not None:
-        _need(P, "P", torch.float32, dev, ndim=2)
-        R = P.shape[1]
-        _like(P, "P", (M, R), torch.float32, dev)
-        _need(U, "U", torch.bfloat16, dev)
-        _like(U, "U", (R, N), torch.bfloat16, dev)
-    _opt(bias, "bias", (N,), torch.bfloat16, dev)
-    y = _output8(y, "y", (M, N), out_dtype, dev)
-    _opt(residual, "residual", (M, N), y.dtype, dev)
+    dev, M, N, K, px, ps, pw, pws = _linear8_operands(xq, xs, wq, ws, 1)
+    R, pp, pu = _low_rank(P, U, ("P", "U"), lambda R: (M, (R, N)), dev)
+    pb = None if bias is None else _fits(bias, "bias", (N,), torch.bfloat16, dev)
+    shape = (M, N)
+    dt, y, py = _output8(y, "y", shape, out_dtype, dev)
+    pr = None if residual is None else _fits(residual, "residual", shape, dt, dev)
+    pz = None
     if z is not None or want_z:
-        z = _like(z, "z", (M, N), torch.bfloat16, dev)
-    _launch(L.ft_linear8_fwd, dev, _ptr(xq), _ptr(xs), M, K, _ptr(wq), _ptr(ws), N, _ptr(P), R, _ptr(U), _ptr(bias), act,
-            _ptr(residual), _ptr(z), _ptr(y), FT_F32 if y.dtype == torch.float32 else FT_BF16)
+        z, pz = _out(z, "z", shape, torch.bfloat16, dev)
+    _launch(load().ft_linear8_fwd, dev, px, ps, M, K, pw, pws, N, pp, R, pu, pb, act, pr, pz, py,
+            FT_F32 if dt is torch.float32 else FT_BF16)
     return y if z is None else (y, z)
 
 
@@ -695,18 +729,12 @@ def ft_linear8_bwd_input(gq, gs, wq, ws, Qp=None, D=None, z=None, act=FT_ACT_NON
     """dx [M, K] = (DQ(gq) DQ(wq) + Qp D^T) * act'(z) + residual on MXFP8
     gradients; z [M, K] bf16 is the saved input of the activation in front of the
     layer, residual has dx's type and may be dx."""
-    L = load()
-    dev, M, N, K = _linear8_operands(gq, gs, wq, ws, True)
-    R = 0
-    if Qp is not None or D is not None:
-        _need(Qp, "Qp", torch.float32, dev, ndim=2)
-        R = Qp.shape[1]
-        _like(Qp, "Qp", (M, R), torch.float32, dev)
-        _need(D, "D", torch.bfloat16, dev)
-        _like(D, "D", (K, R), torch.bfloat16, dev)
-    _opt(z, "z", (M, K), torch.bfloat16, dev)
-    dx = _output8(dx, "dx", (M, K), out_dtype, dev)
-    _opt(residual, "residual", (M, K), dx.dtype, dev)
-    _launch(L.ft_linear8_bwd_input, dev, _ptr(gq), _ptr(gs), M, N, _ptr(wq), _ptr(ws), K, _ptr(Qp), R, _ptr(D), _ptr(z),
-            act, _ptr(residual), _ptr(dx), FT_F32 if dx.dtype == torch.float32 else FT_BF16)
+    dev, M, N, K, pg, ps, pw, pws = _linear8_operands(gq, gs, wq, ws, 0)
+    R, pp, pd = _low_rank(Qp, D, ("Qp", "D"), lambda R: (M, (K, R)), dev)
+    shape = (M, K)
+    pz = None if z is None else _fits(z, "z", shape, torch.bfloat16, dev)
+    dt, dx, px = _output8(dx, "dx", shape, out_dtype, dev)
+    pr = None if residual is None else _fits(residual, "residual", shape, dt, dev)
+    _launch(load().ft_linear8_bwd_input, dev, pg, ps, M, N, pw, pws, K, pp, R, pd, pz, act, pr, px,
+            FT_F32 if dt is torch.float32 else FT_BF16)
     return dx

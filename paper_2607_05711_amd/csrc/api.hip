@@ -518,14 +518,14 @@ int ftx_linear8_tile(int bwd, int64_t M, int64_t N, int64_t K) {
 ft_status ftx_linear8_fwd(int tile, const uint8_t* xq, const uint8_t* xs, int64_t M, int64_t K, const uint8_t* wq,
                           const uint8_t* ws, int64_t N, const float* P, int32_t R, const void* U, const void* bias,
                           ft_act act, const void* residual, void* z, void* y, ft_dtype y_dtype, hipStream_t stream) {
-  if (tile != 64 && tile != 128 && tile != 256 && !(tile == 1 && M <= ft::kRowsMx8Max))
+  if (tile != 64 && tile != 128 && tile != 192 && tile != 256 && !(tile == 1 && M <= ft::kRowsMx8Max))
     return fail(FT_ERR_UNSUPPORTED, "tile = %d", tile);
   return linear8(false, tile, xq, xs, M, N, K, wq, ws, P, R, U, bias, act, residual, z, y, y_dtype, stream);
 }
 ft_status ftx_linear8_bwd_input(int tile, const uint8_t* gq, const uint8_t* gs, int64_t M, int64_t N, const uint8_t* wq,
                                 const uint8_t* ws, int64_t K, const float* Qp, int32_t R, const void* D, const void* z,
                                 ft_act act, const void* residual, void* dx, ft_dtype dx_dtype, hipStream_t stream) {
-  if (tile != 64 && tile != 128 && tile != 256) return fail(FT_ERR_UNSUPPORTED, "tile = %d", tile);
+  if (tile != 64 && tile != 128 && tile != 192 && tile != 256) return fail(FT_ERR_UNSUPPORTED, "tile = %d", tile);
   return linear8(true, tile, gq, gs, M, N, K, wq, ws, Qp, R, D, nullptr, act, residual, const_cast<void*>(z), dx, dx_dtype,
                  stream);
 }

@@ -122,7 +122,7 @@ struct MxArgs {
   void* out;
 };
 bool gemm_mx8_supported(bool bwd, int M, int N, int K, int R);
-// Which output tile: 256 (256x256), 128 (128x128) or 64 (64x128).
+// Which output tile: 256 (256x256), 192 (192x256), 128 (128x128) or 64 (64x128).
 int gemm_mx8_tile(bool bwd, int M, int N, int K);
 hipError_t launch_gemm_mx8(bool bwd, int tile, const MxArgs& a, int act, bool out_f32, hipStream_t st);
 hipError_t launch_gemm_mx8_bf16(bool bwd, int tile, const MxArgs& a, int act, hipStream_t st);

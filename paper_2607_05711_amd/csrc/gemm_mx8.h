@@ -45,9 +45,10 @@ struct MxGeom {
   static constexpr int OFF_S = OFF_W + TN * (XK / 2);   // scales of the X rows, 4 bytes each
   static constexpr int SLOT = OFF_S + TM * 4;
   static constexpr int XL = TM / 32, WL = TN / 64, LOADS = XL + WL + 1;   // per wave and stage
-  static constexpr int MT = TM / 64, NT = TN / 64;      // 32x32 tiles per wave
+  static constexpr int WR = TM / 2, WC = TN / 2;        // rows and columns of a wave
+  static constexpr int MT = WR / 32, NT = WC / 32;      // 32x32 tiles per wave
+  static constexpr int STG = 4 * 2 * 32 * (64 * 4 + 16);   // the epilogue's staging rows (in the ring and the scales)
   static constexpr int NS = TM == 64 ? 4 : 3;           // ring slots
-  static constexpr int STG = 4 * 32 * (64 * 4 + 16);    // the epilogue's staging rows (in the ring)
 };
 
 template <int V> struct IC8 { static constexpr int value = V; };
@@ -71,7 +72,7 @@ __host__ __device__ inline int mx_slab(int tn, int nst) { return (tn / 32 * 4 * 
 }  // namespace
 
 template <bool BWD, int TM, int TN, int ACT, bool F32>
-__global__ __launch_bounds__(256, TM == 256 ? 1 : 2) void k_gemm_mx8(
+__global__ __launch_bounds__(256, TM > 128 ? 1 : 2) void k_gemm_mx8(
     const uint8_t* __restrict__ X, const uint8_t* __restrict__ Xs, const uint8_t* __restrict__ Wq,
     const uint8_t* __restrict__ Ws, int M, int N, int K, const float* __restrict__ P, int R,
     const uint16_t* __restrict__ LR, const uint16_t* __restrict__ bias, uint16_t* z, const void* res, void* out,
@@ -107,9 +108,6 @@ __global__ __launch_bounds__(256, TM == 256 ? 1 : 2) void k_gemm_mx8(
                      : rsrc_words(Wq + (size_t)n0 * ldw, (uint32_t)ncol * ldw);
   const int nst = (KR + XK - 1) / XK, nlr = (R + XLR - 1) / XLR, total = nst + nlr;
   const v4i rxs = rsrc_words(Xs + (size_t)m0 * 4, (uint32_t)(((size_t)(nst - 1) * M + nrow) * 4));
-  const v4i rp = rsrc_words(P + (R ? (size_t)m0 * R : 0), (uint32_t)nrow * R * 4);
-  const v4i rl = BWD ? rsrc_words(LR + (R ? (size_t)n0 * R : 0), (uint32_t)ncol * R * 2)
-                     : rsrc_words(LR, (uint32_t)NO * R * 2);
   const uint32_t lds0 = lds_addr(mxlds);
   const int off_slab = NS * G::SLOT;
 
@@ -170,7 +168,8 @@ __global__ __launch_bounds__(256, TM == 256 ? 1 : 2) void k_gemm_mx8(
       const int q = u - nst, left = u < total ? R - q * XLR : 0;   // low-rank columns from this stage on
       if constexpr (i < G::XL) {
         const int r = (wave * G::XL + i) * 8 + r8, c = c8 ^ (i & 1);
-        dma16(rp, base + (wave * G::XL + i) * 1024, 4 * c < left && r < nrow ? (uint32_t)r * R * 4 + c * 16 : kOobOffset,
+        const v4i rp = rsrc_words(P + (size_t)m0 * R, (uint32_t)nrow * R * 4);
+        dma16(u < total ? rp : rx, base + (wave * G::XL + i) * 1024, 4 * c < left && r < nrow ? (uint32_t)r * R * 4 + c * 16 : kOobOffset,
               u < total ? (uint32_t)q * 128 : 0u);
       } else if constexpr (i < G::XL + G::WL) {
         const int ins = wave * G::WL + i - G::XL;
@@ -185,61 +184,52 @@ __global__ __launch_bounds__(256, TM == 256 ? 1 : 2) void k_gemm_mx8(
           if (k < ncol && 8 * c < left) off = (uint32_t)k * R * 2 + c * 16;
           so = u < total ? (uint32_t)q * 64 : 0u;
         }
-        dma16(rl, base + G::OFF_W + ins * 1024, off, so);
+        const v4i rl = BWD ? rsrc_words(LR + (size_t)n0 * R, (uint32_t)ncol * R * 2) : rsrc_words(LR, (uint32_t)NO * R * 2);
+        dma16(u < total ? rl : rw, base + G::OFF_W + ins * 1024, off, so);
       } else {
         dma4(rxs, base + G::OFF_S + sseg * 256, kOobOffset, 0);
       }
     }
   };
 
-  // ---------------- weight scales into LDS, the first stages' loads
+  // ---------------- the first stages' loads, weight scales into LDS
   // forward [TN / 32 tiles][4 nst blocks], backward [4 nst blocks][TN / 32 tiles]
-  {
-    constexpr int TB = TN / 32;
-    if ((nwkb & 3) == 0) {
-      const int dw = TB * nst;                           // dwords
-      for (int i = tid; i < dw; i += 256) {
-        uint32_t d = 0;
-        if constexpr (!BWD) {
-          const int j = i / nst, b = 4 * (i - j * nst), nb = (n0 >> 5) + j;
-          if (nb < (N >> 5) && b < nwkb) d = *(const uint32_t*)(Ws + (size_t)nb * nwkb + b);
-        } else {
-          const int b = i / (TB / 4), kb = (n0 >> 5) + 4 * (i % (TB / 4));
-          if (b < nkb && kb < nwkb) d = *(const uint32_t*)(Ws + (size_t)b * nwkb + kb);
-        }
-        *(uint32_t*)(mxlds + off_slab + 4 * i) = d;
-      }
-    } else {                                             // rows that are not 4-byte aligned
-      for (int i = tid; i < TB * 4 * nst; i += 256) {
-        const int j = BWD ? i % TB : i / (4 * nst), b = BWD ? i / TB : i - j * 4 * nst;
-        const int nb = (n0 >> 5) + j;
-        const bool in = b < nkb && nb < (NO >> 5);
-        mxlds[off_slab + i] = in ? Ws[BWD ? (size_t)b * nwkb + nb : (size_t)nb * nwkb + b] : (uint8_t)0;
-      }
+  constexpr int TB = TN / 32;
+  const int nfull = KR / XK;
+  auto scale_dword = [&](int i) {                        // rows that are whole dwords
+    uint32_t d = 0;
+    if constexpr (!BWD) {
+      const int j = i / nst, b = 4 * (i - j * nst), nb = (n0 >> 5) + j;
+      if (i < TB * nst && nb < (N >> 5) && b < nwkb) d = *(const uint32_t*)(Ws + (size_t)nb * nwkb + b);
+    } else {
+      const int b = i / (TB / 4), kb = (n0 >> 5) + 4 * (i % (TB / 4));
+      if (b < nkb && kb < nwkb) d = *(const uint32_t*)(Ws + (size_t)b * nwkb + kb);
+    }
+    return d;
+  };
+  const bool dwords = (nwkb & 3) == 0;
+  const uint32_t first = dwords ? scale_dword(tid) : 0u;   // (in flight behind the loads below)
+#pragma unroll 1
+  for (int u = 0; u < NS; u++) {
+    if (u < nfull) static_for<G::LOADS>([&](auto ic) { load_full(ic, u, lds0 + (uint32_t)u * G::SLOT); });
+    else static_for<G::LOADS>([&](auto ic) { load_any(ic, u, lds0 + (uint32_t)u * G::SLOT); });
+  }
+  if (dwords) {
+    if (tid < TB * nst) *(uint32_t*)(mxlds + off_slab + 4 * tid) = first;
+    for (int i = tid + 256; i < TB * nst; i += 256) *(uint32_t*)(mxlds + off_slab + 4 * i) = scale_dword(i);
+  } else {                                               // rows that are not 4-byte aligned
+    for (int i = tid; i < TB * 4 * nst; i += 256) {
+      const int j = BWD ? i % TB : i / (4 * nst), b = BWD ? i / TB : i - j * 4 * nst;
+      const int nb = (n0 >> 5) + j;
+      const bool in = b < nkb && nb < (NO >> 5);
+      mxlds[off_slab + i] = in ? Ws[BWD ? (size_t)b * nwkb + nb : (size_t)nb * nwkb + b] : (uint8_t)0;
     }
   }
-#pragma unroll 1
-  for (int u = 0; u < NS; u++) static_for<G::LOADS>([&](auto ic) { load_any(ic, u, lds0 + (uint32_t)u * G::SLOT); });
-
-  // accumulators start at the bias of their columns
   v16f acc[MT][NT];
-  {
-    const __amdgpu_buffer_rsrc_t rb = make_rsrc(bias, !BWD && bias ? (uint32_t)N * 2 : 0u);
 #pragma unroll
-    for (int j = 0; j < NT; j++)
+  for (int i = 0; i < MT; i++)
 #pragma unroll
-      for (int q = 0; q < 4; q++) {
-        v2i bb = {0, 0};
-        if constexpr (!BWD)
-          bb = __builtin_bit_cast(v2i, __builtin_amdgcn_raw_buffer_load_b64(rb, (n0 + wn * (TN / 2) + 32 * j + 8 * q + 4 * h) * 2, 0, 0));
-        const float b4[4] = {bf16_to_f32((uint32_t)bb[0] & 0xFFFFu), bf16_to_f32((uint32_t)bb[0] >> 16),
-                             bf16_to_f32((uint32_t)bb[1] & 0xFFFFu), bf16_to_f32((uint32_t)bb[1] >> 16)};
-#pragma unroll
-        for (int i = 0; i < MT; i++)
-#pragma unroll
-          for (int e = 0; e < 4; e++) acc[i][j][4 * q + e] = b4[e];
-      }
-  }
+    for (int j = 0; j < NT; j++) acc[i][j] = v16f{};
 
   // ---------------- fragment reads, one LDS read (two for the backward's weight) an op
   const int sw_r = swz128(r32), sw_w = swz64(r32), sw_t = swz64(t16), sw_t8 = (t16 >> 1) & 7;
@@ -247,12 +237,12 @@ __global__ __launch_bounds__(256, TM == 256 ? 1 : 2) void k_gemm_mx8(
   struct Scales { uint32_t x[MT], w[BWD ? 2 : NT]; };
   auto read_x = [&](auto oc, const uint8_t* base, int kk, Frags& f) {
     constexpr int i = decltype(oc)::value >> 1, e = decltype(oc)::value & 1;
-    f.x[i][e] = *(const v4i*)(base + (wm * (TM / 2) + i * 32 + r32) * XK + (((4 * kk + 2 * e + h) ^ sw_r) << 4));
+    f.x[i][e] = *(const v4i*)(base + (wm * G::WR + i * 32 + r32) * XK + (((4 * kk + 2 * e + h) ^ sw_r) << 4));
   };
   auto read_w = [&](auto oc, const uint8_t* base, int kk, Frags& f) {
     constexpr int j = decltype(oc)::value;
     if constexpr (!BWD) {
-      f.w[j] = *(const v4i*)(base + G::OFF_W + (wn * (TN / 2) + j * 32 + r32) * 64 + (((2 * kk + h) ^ sw_w) << 4));
+      f.w[j] = *(const v4i*)(base + G::OFF_W + (wn * G::WC + j * 32 + r32) * 64 + (((2 * kk + h) ^ sw_w) << 4));
     } else {
       const int c = (wn * NT + j) ^ (TN == 256 ? sw_t8 : sw_t);
       const uint8_t* p = base + G::OFF_W + (kk * 64 + 32 * h + t16) * (TN / 2) + (c << 4) + 8 * (g16 & 1);
@@ -271,7 +261,7 @@ __global__ __launch_bounds__(256, TM == 256 ? 1 : 2) void k_gemm_mx8(
     constexpr int o = decltype(oc)::value;
     if constexpr (o < MT) {
       const uint32_t keep = s == nst - 1 ? keep_last : 0xFFFFFFFFu;
-      const uint32_t d = *(const uint32_t*)(base + G::OFF_S + (wm * (TM / 2) + o * 32 + r32) * 4);
+      const uint32_t d = *(const uint32_t*)(base + G::OFF_S + (wm * G::WR + o * 32 + r32) * 4);
       f.x[o] = ((d & keep) | (0x7F7F7F7Fu & ~keep)) >> (8 * h);
     } else if constexpr (!BWD) {
       f.w[o - MT] = *(const uint32_t*)(mxlds + off_slab + ((wn * NT + o - MT) * nst + s) * 4) >> (8 * h);
@@ -314,7 +304,8 @@ __global__ __launch_bounds__(256, TM == 256 ? 1 : 2) void k_gemm_mx8(
   static_for<SOPS>([&](auto oc) { read_op(oc, mxlds, 0, 0, f0, sc); });
   int slot = 0;
   constexpr int MF = MT * NT;
-  auto body = [&](int s, auto fullc) {
+  // KIND of stage s + NS: 0 a whole one of X and W, 1 any other, 2 none.
+  auto body = [&](int s, auto kindc) {
     const int next = slot + 1 == NS ? 0 : slot + 1;
     const uint8_t* here = mxlds + slot * G::SLOT;
     const uint8_t* there = mxlds + next * G::SLOT;
@@ -328,7 +319,8 @@ __global__ __launch_bounds__(256, TM == 256 ? 1 : 2) void k_gemm_mx8(
       });
       __builtin_amdgcn_sched_barrier(0);
     });
-    publish(IC8<NS - 2>{});
+    constexpr int KIND = decltype(kindc)::value;
+    publish(IC8<KIND == 2 ? 0 : NS - 2>{});
     const int sn = min(s + 1, nst - 1);   // unused when stage s + 1 is a low-rank one
     static_for<MF>([&](auto tc) {
       constexpr int t = decltype(tc)::value;
@@ -336,22 +328,24 @@ __global__ __launch_bounds__(256, TM == 256 ? 1 : 2) void k_gemm_mx8(
       static_for<(t + 1) * SOPS / MF - t * SOPS / MF>([&](auto e) {
         read_op(IC8<t * SOPS / MF + decltype(e)::value>{}, there, 0, sn, f0, scn);
       });
-      static_for<(t + 1) * G::LOADS / MF - t * G::LOADS / MF>([&](auto e) {
-        constexpr int i = t * G::LOADS / MF + decltype(e)::value;
-        if constexpr (decltype(fullc)::value != 0) load_full(IC8<i>{}, s + NS, dst);
-        else load_any(IC8<i>{}, s + NS, dst);
-      });
+      if constexpr (KIND != 2)
+        static_for<(t + 1) * G::LOADS / MF - t * G::LOADS / MF>([&](auto e) {
+          constexpr int i = t * G::LOADS / MF + decltype(e)::value;
+          if constexpr (KIND == 0) load_full(IC8<i>{}, s + NS, dst);
+          else load_any(IC8<i>{}, s + NS, dst);
+        });
       __builtin_amdgcn_sched_barrier(0);
     });
     sc = scn;
     slot = next;
   };
-  const int nfull = KR / XK;
   int s = 0;
 #pragma unroll 1
-  for (; s + NS < nfull; s++) body(s, IC8<1>{});
+  for (; s + NS < nfull; s++) body(s, IC8<0>{});
 #pragma unroll 1
-  for (; s < nst; s++) body(s, IC8<0>{});
+  for (; s < nst && s + NS < total; s++) body(s, IC8<1>{});
+#pragma unroll 1
+  for (; s < nst; s++) body(s, IC8<2>{});
 
   // ---------------- low-rank stages: 16 columns at a time, P in two bf16 terms (F32: three)
   const int jj = t16 >> 2, qq = t16 & 3;
@@ -360,12 +354,12 @@ __global__ __launch_bounds__(256, TM == 256 ? 1 : 2) void k_gemm_mx8(
 #pragma unroll
     for (int j = 0; j < NT; j++) {
       if constexpr (!BWD) {
-        const int n = wn * (TN / 2) + j * 32 + 16 * (g16 & 1) + 4 * qq, row = 16 * c + 8 * h + jj;
+        const int n = wn * G::WC + j * 32 + 16 * (g16 & 1) + 4 * qq, row = 16 * c + 8 * h + jj;
         const int ch = (n >> 3) ^ (2 * (row & 3));   // row + 4 has the same swizzle
         const uint8_t* p = base + G::OFF_W + row * (TN * 2) + (ch << 4) + ((n >> 2) & 1) * 8;
         b[j] = make_v8bf(lds_read_tr16((const FT_LDS void*)p), lds_read_tr16((const FT_LDS void*)(p + 4 * TN * 2)));
       } else {
-        b[j] = __builtin_bit_cast(v8bf, *(const v4i*)(base + G::OFF_W + (wn * (TN / 2) + j * 32 + r32) * 64 + (((2 * c + h) ^ sw_w) << 4)));
+        b[j] = __builtin_bit_cast(v8bf, *(const v4i*)(base + G::OFF_W + (wn * G::WC + j * 32 + r32) * 64 + (((2 * c + h) ^ sw_w) << 4)));
       }
     }
 #pragma unroll
@@ -374,7 +368,7 @@ __global__ __launch_bounds__(256, TM == 256 ? 1 : 2) void k_gemm_mx8(
       v4i part[F32 ? 3 : 2];              // terms of P: 16 significant bits, or 24
 #pragma unroll
       for (int e = 0; e < 2; e++)
-        x[e] = *(const v4f*)(base + (wm * (TM / 2) + i * 32 + r32) * 128 + (((4 * c + 2 * h + e) ^ sw_r) << 4));
+        x[e] = *(const v4f*)(base + (wm * G::WR + i * 32 + r32) * 128 + (((4 * c + 2 * h + e) ^ sw_r) << 4));
 #pragma unroll
       for (int e = 0; e < 4; e++) {
         const float a = x[e >> 1][2 * (e & 1)], d = x[e >> 1][2 * (e & 1) + 1];
@@ -399,8 +393,8 @@ __global__ __launch_bounds__(256, TM == 256 ? 1 : 2) void k_gemm_mx8(
     const uint8_t* base = mxlds + slot * G::SLOT;
     lr_half(base, 0);
     if (R - (s - nst) * XLR > 16) lr_half(base, 1);
-    publish(IC8<NS - 2>{});
-    static_for<G::LOADS>([&](auto ic) { load_any(ic, s + NS, lds0 + (uint32_t)slot * G::SLOT); });
+    publish(IC8<0>{});
+    if (s + NS < total) static_for<G::LOADS>([&](auto ic) { load_any(ic, s + NS, lds0 + (uint32_t)slot * G::SLOT); });
     slot = slot + 1 == NS ? 0 : slot + 1;
   }
   wait_vm<0>();   // zeros of stages past the end must not land in the epilogue's LDS
@@ -409,107 +403,148 @@ __global__ __launch_bounds__(256, TM == 256 ? 1 : 2) void k_gemm_mx8(
   // ---------------- epilogue: 32 rows x 64 columns at a time through the wave's own LDS
   // Eight lanes hold 64 columns of a row, eight each, so that every global
   // access is a whole 128-byte line of a row (256 bytes in fp32).  Everything
-  // is fp32 until the one rounding of each output.
-  constexpr int SROW = 64 * 4 + 16;
-  uint8_t* stg = mxlds + wave * (32 * SROW);
+  // is fp32 until the one rounding of each output.  Two staging buffers: a
+  // pass's accumulators are written while the one before is on its way out, and
+  // what a pass reads from memory is loaded in front of the stores of the pass
+  // before (the counter that loads wait on counts stores too).  One pass's code
+  // for all of them, the accumulators chosen by a switch: run once per tile,
+  // unrolled code would be fetched from memory.
+  constexpr int SROW = 64 * 4 + 16, PASSES = MT * NT / 2, JP = NT / 2;
+  constexpr bool ZIN = BWD && ACT != ACT_NONE;
   constexpr int es = F32 ? 4 : 2;
+  uint8_t* stg = mxlds + wave * (2 * 32 * SROW);
   const size_t tile0 = (size_t)m0 * NO + n0;
   const uint32_t span = (uint32_t)(nrow - 1) * NO + ncol;   // elements from the tile's first to its last
   const __amdgpu_buffer_rsrc_t ro = make_rsrc((uint8_t*)out + tile0 * es, span * es);
   const __amdgpu_buffer_rsrc_t rr = make_rsrc(res ? (const uint8_t*)res + tile0 * es : nullptr, res ? span * es : 0u);
+  const __amdgpu_buffer_rsrc_t rb = make_rsrc(bias, !BWD && bias ? (uint32_t)N * 2 : 0u);   // (no bias reads zeros)
   const __amdgpu_buffer_rsrc_t rz = make_rsrc(z ? z + tile0 : nullptr, z ? span * 2 : 0u);
-#pragma unroll
-  for (int i = 0; i < MT; i++)
-#pragma unroll
-    for (int jp = 0; jp < NT / 2; jp++) {
-      // element offset of this lane's eight columns in the tile, or none
-      uint32_t at[4];
+  // Element offset of this lane's eight columns in the wave's first row; rows
+  // past the tile's lie past the buffers' ends, columns past it are marked.
+  const int lrow = lane >> 3, lcol = wn * G::WC + (lane & 7) * 8;
+  auto at = [&](int pass, int it) {
+    const int c = lcol + 64 * (pass % JP), r = wm * G::WR + 32 * (pass / JP) + 8 * it;
+    return c < ncol ? (uint32_t)(r + lrow) * NO + c : kOobOffset;
+  };
+  struct Pass { v4i z[ZIN ? 4 : 1], r[4][F32 ? 2 : 1]; };
+  auto load_pass = [&](int pass, Pass& d) {
+    if constexpr (ZIN) {
 #pragma unroll
       for (int it = 0; it < 4; it++) {
-        const int r = wm * (TM / 2) + 32 * i + it * 8 + (lane >> 3), c = wn * (TN / 2) + 64 * jp + (lane & 7) * 8;
-        at[it] = r < nrow && c < ncol ? (uint32_t)r * NO + c : kOobOffset;
+        const uint32_t a = at(pass, it);
+        d.z[it] = __builtin_bit_cast(v4i, __builtin_amdgcn_raw_buffer_load_b128(rz, a == kOobOffset ? a : a * 2, 0, 0));
       }
-      v4i zv[4], rv[4][2];
-      if (BWD && ACT != ACT_NONE) {
+    }
+    if (res) {
 #pragma unroll
-        for (int it = 0; it < 4; it++)
-          zv[it] = __builtin_bit_cast(v4i, __builtin_amdgcn_raw_buffer_load_b128(rz, at[it] == kOobOffset ? kOobOffset : at[it] * 2, 0, 0));
+      for (int it = 0; it < 4; it++) {
+        const uint32_t a = at(pass, it), o = a == kOobOffset ? a : a * es;
+        d.r[it][0] = __builtin_bit_cast(v4i, __builtin_amdgcn_raw_buffer_load_b128(rr, o, 0, 0));
+        if constexpr (F32) d.r[it][1] = __builtin_bit_cast(v4i, __builtin_amdgcn_raw_buffer_load_b128(rr, o, 16, 0));
+      }
+    }
+  };
+  auto stage = [&](int pass) {
+    uint8_t* to = stg + (pass & 1) * (32 * SROW) + r32 * SROW + 16 * h;
+    static_for<PASSES>([&](auto pc) {
+      constexpr int p = decltype(pc)::value;
+      if (pass == p) {
+#pragma unroll
+        for (int jh = 0; jh < 2; jh++)
+#pragma unroll
+          for (int q = 0; q < 4; q++) {
+            const v16f& a = acc[p / JP][2 * (p % JP) + jh];
+            *(v4f*)(to + (32 * jh + 8 * q) * 4) = v4f{a[4 * q], a[4 * q + 1], a[4 * q + 2], a[4 * q + 3]};
+          }
+        asm volatile("; pass %0" ::"n"(p));
+      }
+    });
+  };
+  float bf[JP][8];
+#pragma unroll
+  for (int jp = 0; jp < JP; jp++)
+    if constexpr (!BWD)
+      unpack_bf16x8(__builtin_bit_cast(v4i, __builtin_amdgcn_raw_buffer_load_b128(rb, (n0 + lcol + 64 * jp) * 2, 0, 0)), bf[jp]);
+  Pass cur, nxt;
+  load_pass(0, cur);
+  stage(0);
+  auto run_pass = [&](int pass, auto jc) {
+    __builtin_amdgcn_s_waitcnt(0xc07f);                 // the wave reads back only its own rows
+    asm volatile("" ::: "memory");
+    const uint8_t* from = stg + (pass & 1) * (32 * SROW) + lrow * SROW + (lane & 7) * 32;
+    v4f v[4][2];
+#pragma unroll
+    for (int it = 0; it < 4; it++) {
+      v[it][0] = *(const v4f*)(from + it * 8 * SROW);
+      v[it][1] = *(const v4f*)(from + it * 8 * SROW + 16);
+    }
+    if (pass + 1 < PASSES) {
+      load_pass(pass + 1, nxt);
+      stage(pass + 1);
+    }
+#pragma unroll
+    for (int it = 0; it < 4; it++) {
+      float f[8] = {v[it][0][0], v[it][0][1], v[it][0][2], v[it][0][3], v[it][1][0], v[it][1][1], v[it][1][2], v[it][1][3]};
+      const uint32_t a = at(pass, it);
+      if constexpr (!BWD) {
+#pragma unroll
+        for (int e = 0; e < 8; e++) f[e] += bf[decltype(jc)::value][e];
+        if (z) __builtin_amdgcn_raw_buffer_store_b128(pack_bf16x8(f), rz, a == kOobOffset ? a : a * 2, 0, 0);
+#pragma unroll
+        for (int e = 0; e < 8; e++) f[e] = act_fn<ACT>(f[e]);
+      } else if constexpr (ZIN) {
+        float zf[8];
+        unpack_bf16x8(cur.z[it], zf);
+#pragma unroll
+        for (int e = 0; e < 8; e++) f[e] *= act_grad<ACT>(zf[e]);
       }
       if (res) {
-#pragma unroll
-        for (int it = 0; it < 4; it++) {
-          const uint32_t o = at[it] == kOobOffset ? kOobOffset : at[it] * es;
-          rv[it][0] = __builtin_bit_cast(v4i, __builtin_amdgcn_raw_buffer_load_b128(rr, o, 0, 0));
-          if (F32) rv[it][1] = __builtin_bit_cast(v4i, __builtin_amdgcn_raw_buffer_load_b128(rr, o, 16, 0));
-        }
-      }
-#pragma unroll
-      for (int jh = 0; jh < 2; jh++)
-#pragma unroll
-        for (int q = 0; q < 4; q++) {
-          const v16f& a = acc[i][2 * jp + jh];
-          *(v4f*)(stg + r32 * SROW + (32 * jh + 8 * q + 4 * h) * 4) = v4f{a[4 * q], a[4 * q + 1], a[4 * q + 2], a[4 * q + 3]};
-        }
-      __builtin_amdgcn_s_waitcnt(0xc07f);               // the wave reads back only its own rows
-#pragma unroll
-      for (int it = 0; it < 4; it++) {
-        const uint8_t* p = stg + (it * 8 + (lane >> 3)) * SROW + (lane & 7) * 32;
-        const v4f lo = *(const v4f*)p, hi = *(const v4f*)(p + 16);
-        float f[8] = {lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
-        const uint32_t o = at[it] == kOobOffset ? kOobOffset : at[it] * es;
-        if constexpr (!BWD) {
-          if (z) __builtin_amdgcn_raw_buffer_store_b128(pack_bf16x8(f), rz, at[it] == kOobOffset ? kOobOffset : at[it] * 2, 0, 0);
-#pragma unroll
-          for (int e = 0; e < 8; e++) f[e] = act_fn<ACT>(f[e]);
-        } else if constexpr (ACT != ACT_NONE) {
-          float zf[8];
-          unpack_bf16x8(zv[it], zf);
-#pragma unroll
-          for (int e = 0; e < 8; e++) f[e] *= act_grad<ACT>(zf[e]);
-        }
-        if (res) {
-          float rf[8];
-          if constexpr (F32) {
-#pragma unroll
-            for (int e = 0; e < 8; e++) rf[e] = __int_as_float(rv[it][e >> 2][e & 3]);
-          } else {
-            unpack_bf16x8(rv[it][0], rf);
-          }
-#pragma unroll
-          for (int e = 0; e < 8; e++) f[e] += rf[e];
-        }
+        float rf[8];
         if constexpr (F32) {
-          __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(v4i, v4f{f[0], f[1], f[2], f[3]}), ro, o, 0, 0);
-          __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(v4i, v4f{f[4], f[5], f[6], f[7]}), ro, o, 16, 0);
+#pragma unroll
+          for (int e = 0; e < 8; e++) rf[e] = __int_as_float(cur.r[it][e >> 2][e & 3]);
         } else {
-          __builtin_amdgcn_raw_buffer_store_b128(pack_bf16x8(f), ro, o, 0, 0);
+          unpack_bf16x8(cur.r[it][0], rf);
         }
+#pragma unroll
+        for (int e = 0; e < 8; e++) f[e] += rf[e];
       }
-      asm volatile("" ::: "memory");                    // the next pass's staging writes stay behind these reads
+      const uint32_t o = a == kOobOffset ? a : a * es;
+      if constexpr (F32) {
+        __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(v4i, v4f{f[0], f[1], f[2], f[3]}), ro, o, 0, 0);
+        __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(v4i, v4f{f[4], f[5], f[6], f[7]}), ro, o, 16, 0);
+      } else {
+        __builtin_amdgcn_raw_buffer_store_b128(pack_bf16x8(f), ro, o, 0, 0);
+      }
     }
+    cur = nxt;
+  };
+#pragma unroll 1
+  for (int i = 0; i < MT; i++) static_for<JP>([&](auto jc) { run_pass(i * JP + decltype(jc)::value, jc); });
 }
 
 template <bool F32>
 hipError_t launch_gemm_mx8_t(bool bwd, int tm, const MxArgs& a, int act, hipStream_t st) {
   const int NO = bwd ? a.K : a.N, nst = ((bwd ? a.N : a.K) + XK - 1) / XK;
-  const int tn = tm == 256 ? 256 : 128;
+  const int tn = tm > 128 ? 256 : 128;
   const int tiles_m = (a.M + tm - 1) / tm, tiles_n = (NO + tn - 1) / tn;
   const unsigned grid = (unsigned)(((long)tiles_m * tiles_n + 7) / 8 * 8);
-#define FT_MX(BW, TM_, TN_, ACT_)                                                                                   \
+#define FT_MX(BW, TM_, TN_, ACT_)                                                                              \
   do {                                                                                                              \
-    using G = MxGeom<TM_, TN_>;                                                                                     \
-    static_assert(G::NS * G::SLOT >= G::STG, "the epilogue's rows lie in the ring");                                \
-    k_gemm_mx8<BW, TM_, TN_, ACT_, F32><<<grid, 256, (size_t)G::NS * G::SLOT + mx_slab(TN_, nst), st>>>(            \
+    using G = MxGeom<TM_, TN_>;                                                                                \
+    const size_t lds = std::max((size_t)G::NS * G::SLOT + mx_slab(TN_, nst), (size_t)G::STG);                       \
+    k_gemm_mx8<BW, TM_, TN_, ACT_, F32><<<grid, 256, lds, st>>>(                                          \
         a.x, a.xs, a.wq, a.ws, a.M, a.N, a.K, a.P, a.R, a.lr, a.bias, a.z, a.res, a.out, tiles_m, tiles_n);         \
   } while (0)
 #define FT_MX_ACT(BW, TM_, TN_)                                   \
-  do {                                                            \
+  do {                                                                 \
     if (act == ACT_GELU) FT_MX(BW, TM_, TN_, ACT_GELU);           \
     else if (act == ACT_SILU) FT_MX(BW, TM_, TN_, ACT_SILU);      \
     else if (act == ACT_RELU) FT_MX(BW, TM_, TN_, ACT_RELU);      \
     else FT_MX(BW, TM_, TN_, ACT_NONE);                           \
   } while (0)
   if (tm == 256) { if (!bwd) FT_MX_ACT(false, 256, 256); else FT_MX_ACT(true, 256, 256); }
+  else if (tm == 192) { if (!bwd) FT_MX_ACT(false, 192, 256); else FT_MX_ACT(true, 192, 256); }
   else if (tm == 128) { if (!bwd) FT_MX_ACT(false, 128, 128); else FT_MX_ACT(true, 128, 128); }
   else { if (!bwd) FT_MX_ACT(false, 64, 128); else FT_MX_ACT(true, 64, 128); }
 #undef FT_MX_ACT

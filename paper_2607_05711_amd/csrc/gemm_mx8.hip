@@ -10,16 +10,32 @@ bool gemm_mx8_supported(bool bwd, int M, int N, int K, int R) {
   return (long)N * K / 2 < lim && KR <= 65536 && NO <= 1 << 20 && (KR + 127) / 128 * 4 * M < lim && NO * std::max(R, 1) * 2 < lim;
 }
 
-// Which tile: the one whose rounds of workgroups cost least.
+// Which tile: the one of the least estimated time, in microseconds: rounds of
+// workgroups (one a CU on the wide tiles, two on the others, whose last round
+// may be of one) of a fixed part, the tile's start and end, and one per stage.
+// Measured and estimated, M x K -> N, 256x256 / 192x256 / 128x128 / 64x128:
+//   4608 x 4096 -> 16384   238 / 233 / 263 / 329    232 / 220 / 275 / 341
+//   4608 x 16384 -> 4096   306 / 247 / 260 / 300    323 / 252 / 278 / 295
+//   18432 x 4096 -> 16384  882 / 943 / 1074 / 1313  835 / 883 / 1100 / 1370
+//   2048 x 4096 -> 4096    44 / 36 / 33 / 43        46 / 37 / 31 / 38
+//   512 x 4096 -> 4096     40 / 32 / 18 / 14        46 / 37 / 17 / 13
 int gemm_mx8_tile(bool bwd, int M, int N, int K) {
-  const long NO = bwd ? K : N, KR = bwd ? N : K;
-  auto tiles = [&](int tm, int tn) { return ((M + tm - 1) / tm) * ((NO + tn - 1) / tn); };
-  const bool big = MxGeom<256, 256>::SLOT * 3 + mx_slab(256, (int)((KR + 127) / 128)) <= kCuLdsBytes;
-  const double c256 = (double)((tiles(256, 256) + 255) / 256) * 4.0;
-  const double c128 = (double)((tiles(128, 128) + 255) / 256) * 1.3;
-  const double c64 = (double)((tiles(64, 128) + 255) / 256) * 0.8;
-  if (big && c256 <= c128 && c256 <= c64) return 256;
-  return c128 <= c64 ? 128 : 64;
+  const long NO = bwd ? K : N, nst = ((bwd ? N : K) + 127) / 128;
+  const struct { int tm, tn, cap; double fix, stage, fix1, stage1; size_t slot; } t[] = {
+      {256, 256, 256, 8.0, 1.2, 8.0, 1.2, MxGeom<256, 256>::SLOT},
+      {192, 256, 256, 7.0, 0.93, 7.0, 0.93, MxGeom<192, 256>::SLOT},
+      {128, 128, 512, 4.0, 0.83, 4.0, 0.42, 0},
+      {64, 128, 512, 4.0, 0.47, 4.0, 0.27, 0}};
+  int best = 64;
+  double least = 1e30;
+  for (const auto& g : t) {
+    if (g.slot * 3 + mx_slab(g.tn, (int)nst) > (size_t)kCuLdsBytes) continue;
+    const long n = ((M + g.tm - 1) / g.tm) * ((NO + g.tn - 1) / g.tn), full = n / g.cap, rest = n % g.cap;
+    const double time = full * (g.fix + g.stage * nst) +
+                        (rest == 0 ? 0.0 : rest <= 256 ? g.fix1 + g.stage1 * nst : g.fix + g.stage * nst);
+    if (time < least) { least = time; best = g.tm; }
+  }
+  return best;
 }
 
 hipError_t launch_gemm_mx8(bool bwd, int tile, const MxArgs& a, int act, bool out_f32, hipStream_t st) {

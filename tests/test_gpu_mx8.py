@@ -306,7 +306,7 @@ def test_linear_few_rows(M, K, N, R, act, residual, f32, on_tile):
     linear_case(M, K, N, R, act, residual, R != 48, False, f32, M + K + N)
 
 
-@pytest.mark.parametrize("tile", [64, 128, 256])
+@pytest.mark.parametrize("tile", [64, 128, 192, 256])
 @pytest.mark.parametrize("back", [False, True])
 @pytest.mark.parametrize("act,residual,f32", [(0, True, False), (2, False, True), (1, True, True), (3, False, False)])
 @pytest.mark.parametrize("M,K,N,R", SIZES)
@@ -348,7 +348,7 @@ def exact_operand(g, M, K):
 
 
 @pytest.mark.parametrize("back", [False, True])
-@pytest.mark.parametrize("tile", [1, 64, 128, 256])
+@pytest.mark.parametrize("tile", [1, 64, 128, 192, 256])
 @pytest.mark.parametrize("M,K,N", [(1, 32, 32), (64, 4096, 96), (37, 160, 288), (63, 96, 544), (300, 1056, 416),
                                    (513, 2080, 1056), (1000, 4096, 256)])
 def test_linear_exact(M, K, N, tile, back, on_tile):
@@ -369,7 +369,7 @@ def test_linear_exact(M, K, N, tile, back, on_tile):
 
 
 @pytest.mark.parametrize("back", [False, True])
-@pytest.mark.parametrize("tile", [1, 64, 128, 256])
+@pytest.mark.parametrize("tile", [1, 64, 128, 192, 256])
 def test_product_groups_of_fp32_results(tile, back, on_tile):
     """Small products beside a large one in the same eight reduction elements: an fp32 result keeps all of them."""
     if tile == 1 and back:
