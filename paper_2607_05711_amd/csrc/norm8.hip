@@ -106,10 +106,12 @@ __global__ __launch_bounds__(256) void k_rmsnorm_q8(const uint16_t* x, const uin
 
 hipError_t launch_rmsnorm_q8(const uint16_t* x, const uint16_t* res, const uint16_t* w, float eps, int rows, int K,
                              uint16_t* h, uint16_t* y, uint8_t* codes, uint8_t* scales, float* rstd, hipStream_t st) {
-  // One wave a row where rows fill the chip (four workgroups a CU) and a row
-  // fits a wave's registers; else a workgroup a row, which shortens the row's
-  // way through one lane.
-  const bool wide = K > 4096 || rows < 4096;
+  // A workgroup a row where rows are long or too few to fill the chip with one
+  // wave each: 4608 x 4096 with every output 26.0 us against 34.8 on one wave a
+  // row (whose 244 registers leave two waves a SIMD); 4608 x 1024 9.1 against 8.3,
+  // 18432 x 1024 without y 25.0 against 21.1, where a workgroup's four waves
+  // would be half idle.
+  const bool wide = K > 2048 || rows < 4096;
   const int nc = (K + (wide ? 2047 : 511)) / (wide ? 2048 : 512);
   const int nwg = (wide ? rows : (rows + 3) / 4);
   const unsigned grid = (unsigned)((nwg + 7) / 8 * 8);
@@ -122,9 +124,7 @@ hipError_t launch_rmsnorm_q8(const uint16_t* x, const uint16_t* res, const uint1
     else FT_NORM(8, 4);
   } else {
     if (nc <= 2) FT_NORM(2, 1);
-    else if (nc <= 4) FT_NORM(4, 1);
-    else if (nc <= 6) FT_NORM(6, 1);
-    else FT_NORM(8, 1);
+    else FT_NORM(4, 1);
   }
 #undef FT_NORM
   return hipGetLastError();
@@ -236,29 +236,35 @@ __global__ __launch_bounds__(256) void k_rmsnorm_bwd(const uint16_t* dy, const u
   }
 }
 
-// dw[k] = sum over the parts: a workgroup takes 32 columns, its 32 groups of 8
-// lanes every 32nd part each, and adds the groups in order.
+// dw[k] = sum over the parts: a workgroup takes 16 columns, its 64 groups of 4
+// lanes every 64th part each, all in flight together, and adds the groups in order.
 __global__ __launch_bounds__(256) void k_rmsnorm_dw(const float* __restrict__ parts, int n, int K, float* __restrict__ dw) {
-  __shared__ float sums[32][33];
-  const int g = threadIdx.x >> 3, j = (threadIdx.x & 7) * 4, col = blockIdx.x * 32 + j;   // K % 32 == 0
+  __shared__ float sums[64][17];
+  const int g = threadIdx.x >> 2, j = (threadIdx.x & 3) * 4, col = blockIdx.x * 16 + j;   // K % 32 == 0
   v4f s = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll 4
-  for (int p = g; p < n; p += 32) s += *(const v4f*)(parts + (size_t)p * K + col);
+#pragma unroll 8
+  for (int p = g; p < n; p += 64) s += *(const v4f*)(parts + (size_t)p * K + col);
 #pragma unroll
   for (int e = 0; e < 4; e++) sums[g][j + e] = s[e];
   __syncthreads();
-  if (threadIdx.x < 32) {
+  if (threadIdx.x < 64) {                            // 16 groups a lane, then the four lanes of a column
+    const int c = threadIdx.x & 15, q = threadIdx.x >> 4;
     float t = 0.f;
 #pragma unroll
-    for (int i = 0; i < 32; i++) t += sums[i][threadIdx.x];
-    dw[blockIdx.x * 32 + threadIdx.x] = t;
+    for (int i = 0; i < 16; i++) t += sums[16 * q + i][c];
+    t += __shfl_xor(t, 16, 64);
+    t += __shfl_xor(t, 32, 64);
+    if (q == 0) dw[blockIdx.x * 16 + c] = t;
   }
 }
 
 namespace {
 struct BwdPlan { bool wide; int nc, groups; };
+// As in the forward; 512 workgroups (two a CU) or fewer, since each leaves a row
+// of partial sums: 4608 x 4096 28.8 us with 512, 31.1 with 768, 32.2 with 1024; 38.4
+// on one wave a row.
 BwdPlan bwd_plan(int rows, int K) {
-  const bool wide = K > 4096 || rows < 2048;
+  const bool wide = K > 2048 || rows < 2048;
   const int units = wide ? rows : (rows + 3) / 4;
   return {wide, (K + (wide ? 2047 : 511)) / (wide ? 2048 : 512), std::min(units, 512)};
 }
@@ -270,7 +276,7 @@ hipError_t launch_rmsnorm_bwd(const uint16_t* dy, const uint16_t* dh, const uint
                               const float* rstd, int rows, int K, uint16_t* dx, float* dw, float* ws, hipStream_t st) {
   const BwdPlan p = bwd_plan(rows, K);
   if (rows == 0) {                                   // a sum over no rows
-    if (dw) k_rmsnorm_dw<<<(unsigned)(K / 32), 256, 0, st>>>(ws, 0, K, dw);
+    if (dw) k_rmsnorm_dw<<<(unsigned)(K / 16), 256, 0, st>>>(ws, 0, K, dw);
     return hipGetLastError();
   }
 #define FT_BWD(NC_, WPR_)                                                                                             \
@@ -285,14 +291,12 @@ hipError_t launch_rmsnorm_bwd(const uint16_t* dy, const uint16_t* dh, const uint
     else FT_BWD(8, 4);
   } else {
     if (p.nc <= 2) FT_BWD(2, 1);
-    else if (p.nc <= 4) FT_BWD(4, 1);
-    else if (p.nc <= 6) FT_BWD(6, 1);
-    else FT_BWD(8, 1);
+    else FT_BWD(4, 1);
   }
 #undef FT_BWD
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || !dw) return e;
-  k_rmsnorm_dw<<<(unsigned)(K / 32), 256, 0, st>>>(ws, p.groups, K, dw);
+  k_rmsnorm_dw<<<(unsigned)(K / 16), 256, 0, st>>>(ws, p.groups, K, dw);
   return hipGetLastError();
 }
 
