@@ -66,13 +66,27 @@ __device__ __forceinline__ v16f mfma_w4x8(v4i w, v8i x, v16f c, int sw, int sx) 
   return __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(a, x, c, 4, 0, SA, sw, SB, sx);
 }
 
+// a / b for 0 <= a < 2^31, b > 0: the quotient of the fp32 values is off by at
+// most 2^-22 of itself; the remainder says by how much.  (A dozen instructions,
+// where the compiler's division takes three dozen, in front of everything else.)
+__device__ __forceinline__ int div_small(int a, int b) {
+  int q = (int)((float)a * __builtin_amdgcn_rcpf((float)b));
+  int r = a - q * b;
+  const int c = (int)((float)r * __builtin_amdgcn_rcpf((float)b));   // what the first quotient missed
+  q += c;
+  r -= c * b;
+  return r < 0 ? q - 1 : r >= b ? q + 1 : q;
+}
+
 // Bytes of LDS that hold the weight's scales: TN / 32 tiles by 4 per stage.
 __host__ __device__ inline int mx_slab(int tn, int nst) { return (tn / 32 * 4 * nst + 15) & ~15; }
 
 }  // namespace
 
-template <bool BWD, int TM, int TN, int ACT, bool F32>
-__global__ __launch_bounds__(256, TM > 128 ? 1 : 2) void k_gemm_mx8(
+// KG groups of four waves take every KG-th stage of the reduction, each with a
+// ring and accumulators of its own, which meet in LDS at the end.
+template <bool BWD, int TM, int TN, int KG, int ACT, bool F32>
+__global__ __launch_bounds__(256 * KG, TM > 128 ? 1 : 2) void k_gemm_mx8(
     const uint8_t* __restrict__ X, const uint8_t* __restrict__ Xs, const uint8_t* __restrict__ Wq,
     const uint8_t* __restrict__ Ws, int M, int N, int K, const float* __restrict__ P, int R,
     const uint16_t* __restrict__ LR, const uint16_t* __restrict__ bias, uint16_t* z, const void* res, void* out,
@@ -89,16 +103,16 @@ __global__ __launch_bounds__(256, TM > 128 ? 1 : 2) void k_gemm_mx8(
   int mt, nt;
   {
     constexpr int GM = 8;
-    const int g = t / (GM * tiles_n), first = g * GM, gm = min(GM, tiles_m - first), w = t - g * GM * tiles_n;
-    mt = first + w % gm;
-    nt = w / gm;
+    const int g = div_small(t, GM * tiles_n), first = g * GM, gm = min(GM, tiles_m - first), w = t - g * GM * tiles_n;
+    nt = gm == GM ? w / GM : div_small(w, gm);
+    mt = first + w - nt * gm;
   }
   const int m0 = mt * TM, n0 = nt * TN;
   const int NO = BWD ? K : N, KR = BWD ? N : K;
   const int nrow = min(TM, M - m0), ncol = min(TN, NO - n0);
   const int ldw = K >> 1, nwkb = K >> 5, nkb = KR >> 5;
   const int tid = threadIdx.x, lane = tid & 63;
-  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int wv = __builtin_amdgcn_readfirstlane(tid >> 6), kg = KG == 1 ? 0 : wv >> 2, wave = wv & 3;
   const int r32 = lane & 31, h = lane >> 5, g16 = lane >> 4, t16 = lane & 15;
   const int wm = wave >> 1, wn = wave & 1;
 
@@ -108,8 +122,9 @@ __global__ __launch_bounds__(256, TM > 128 ? 1 : 2) void k_gemm_mx8(
                      : rsrc_words(Wq + (size_t)n0 * ldw, (uint32_t)ncol * ldw);
   const int nst = (KR + XK - 1) / XK, nlr = (R + XLR - 1) / XLR, total = nst + nlr;
   const v4i rxs = rsrc_words(Xs + (size_t)m0 * 4, (uint32_t)(((size_t)(nst - 1) * M + nrow) * 4));
-  const uint32_t lds0 = lds_addr(mxlds);
-  const int off_slab = NS * G::SLOT;
+  uint8_t* ring = mxlds + kg * (NS * G::SLOT);
+  const uint32_t lds0 = lds_addr(ring);
+  const int off_slab = KG * NS * G::SLOT;
 
   // ---------------- per-lane load offsets within a whole stage
   const int r8 = lane >> 3, c8 = (lane & 7) ^ r8;
@@ -199,7 +214,7 @@ __global__ __launch_bounds__(256, TM > 128 ? 1 : 2) void k_gemm_mx8(
   auto scale_dword = [&](int i) {                        // rows that are whole dwords
     uint32_t d = 0;
     if constexpr (!BWD) {
-      const int j = i / nst, b = 4 * (i - j * nst), nb = (n0 >> 5) + j;
+      const int j = div_small(i, nst), b = 4 * (i - j * nst), nb = (n0 >> 5) + j;
       if (i < TB * nst && nb < (N >> 5) && b < nwkb) d = *(const uint32_t*)(Ws + (size_t)nb * nwkb + b);
     } else {
       const int b = i / (TB / 4), kb = (n0 >> 5) + 4 * (i % (TB / 4));
@@ -210,15 +225,16 @@ __global__ __launch_bounds__(256, TM > 128 ? 1 : 2) void k_gemm_mx8(
   const bool dwords = (nwkb & 3) == 0;
   const uint32_t first = dwords ? scale_dword(tid) : 0u;   // (in flight behind the loads below)
 #pragma unroll 1
-  for (int u = 0; u < NS; u++) {
-    if (u < nfull) static_for<G::LOADS>([&](auto ic) { load_full(ic, u, lds0 + (uint32_t)u * G::SLOT); });
-    else static_for<G::LOADS>([&](auto ic) { load_any(ic, u, lds0 + (uint32_t)u * G::SLOT); });
+  for (int s = 0; s < NS; s++) {
+    const int u = KG * s + kg;
+    if (u < nfull) static_for<G::LOADS>([&](auto ic) { load_full(ic, u, lds0 + (uint32_t)s * G::SLOT); });
+    else static_for<G::LOADS>([&](auto ic) { load_any(ic, u, lds0 + (uint32_t)s * G::SLOT); });
   }
   if (dwords) {
     if (tid < TB * nst) *(uint32_t*)(mxlds + off_slab + 4 * tid) = first;
-    for (int i = tid + 256; i < TB * nst; i += 256) *(uint32_t*)(mxlds + off_slab + 4 * i) = scale_dword(i);
+    for (int i = tid + 256 * KG; i < TB * nst; i += 256 * KG) *(uint32_t*)(mxlds + off_slab + 4 * i) = scale_dword(i);
   } else {                                               // rows that are not 4-byte aligned
-    for (int i = tid; i < TB * 4 * nst; i += 256) {
+    for (int i = tid; i < TB * 4 * nst; i += 256 * KG) {
       const int j = BWD ? i % TB : i / (4 * nst), b = BWD ? i / TB : i - j * 4 * nst;
       const int nb = (n0 >> 5) + j;
       const bool in = b < nkb && nb < (NO >> 5);
@@ -301,14 +317,16 @@ __global__ __launch_bounds__(256, TM > 128 ? 1 : 2) void k_gemm_mx8(
   publish(IC8<NS - 1>{});
   Frags f0, f1;
   Scales sc;
-  static_for<SOPS>([&](auto oc) { read_op(oc, mxlds, 0, 0, f0, sc); });
+  static_for<SOPS>([&](auto oc) { read_op(oc, ring, 0, min(kg, nst - 1), f0, sc); });
   int slot = 0;
   constexpr int MF = MT * NT;
+  // The group's stages: the reduction's kg, kg + KG, ... of nst, then the low-rank ones.
+  const int gfull = (nfull - kg + KG - 1) / KG, gst = (nst - kg + KG - 1) / KG, gtotal = (total - kg + KG - 1) / KG;
   // KIND of stage s + NS: 0 a whole one of X and W, 1 any other, 2 none.
   auto body = [&](int s, auto kindc) {
     const int next = slot + 1 == NS ? 0 : slot + 1;
-    const uint8_t* here = mxlds + slot * G::SLOT;
-    const uint8_t* there = mxlds + next * G::SLOT;
+    const uint8_t* here = ring + slot * G::SLOT;
+    const uint8_t* there = ring + next * G::SLOT;
     const uint32_t dst = lds0 + (uint32_t)slot * G::SLOT;
     Scales scn;
     static_for<MF>([&](auto tc) {
@@ -321,18 +339,18 @@ __global__ __launch_bounds__(256, TM > 128 ? 1 : 2) void k_gemm_mx8(
     });
     constexpr int KIND = decltype(kindc)::value;
     publish(IC8<KIND == 2 ? 0 : NS - 2>{});
-    const int sn = min(s + 1, nst - 1);   // unused when stage s + 1 is a low-rank one
+    const int un = min(KG * (s + 1) + kg, nst - 1);   // unused when stage s + 1 is a low-rank one
     static_for<MF>([&](auto tc) {
       constexpr int t = decltype(tc)::value;
       mfma(IC8<1>{}, tc, f1, sc);
       static_for<(t + 1) * SOPS / MF - t * SOPS / MF>([&](auto e) {
-        read_op(IC8<t * SOPS / MF + decltype(e)::value>{}, there, 0, sn, f0, scn);
+        read_op(IC8<t * SOPS / MF + decltype(e)::value>{}, there, 0, un, f0, scn);
       });
       if constexpr (KIND != 2)
         static_for<(t + 1) * G::LOADS / MF - t * G::LOADS / MF>([&](auto e) {
           constexpr int i = t * G::LOADS / MF + decltype(e)::value;
-          if constexpr (KIND == 0) load_full(IC8<i>{}, s + NS, dst);
-          else load_any(IC8<i>{}, s + NS, dst);
+          if constexpr (KIND == 0) load_full(IC8<i>{}, KG * (s + NS) + kg, dst);
+          else load_any(IC8<i>{}, KG * (s + NS) + kg, dst);
         });
       __builtin_amdgcn_sched_barrier(0);
     });
@@ -341,11 +359,11 @@ __global__ __launch_bounds__(256, TM > 128 ? 1 : 2) void k_gemm_mx8(
   };
   int s = 0;
 #pragma unroll 1
-  for (; s + NS < nfull; s++) body(s, IC8<0>{});
+  for (; s + NS < gfull; s++) body(s, IC8<0>{});
 #pragma unroll 1
-  for (; s < nst && s + NS < total; s++) body(s, IC8<1>{});
+  for (; s < gst && s + NS < gtotal; s++) body(s, IC8<1>{});
 #pragma unroll 1
-  for (; s < nst; s++) body(s, IC8<2>{});
+  for (; s < gst; s++) body(s, IC8<2>{});
 
   // ---------------- low-rank stages: 16 columns at a time, P in two bf16 terms (F32: three)
   const int jj = t16 >> 2, qq = t16 & 3;
@@ -389,16 +407,37 @@ __global__ __launch_bounds__(256, TM > 128 ? 1 : 2) void k_gemm_mx8(
     }
   };
 #pragma unroll 1
-  for (; s < total; s++) {
-    const uint8_t* base = mxlds + slot * G::SLOT;
+  for (; s < gtotal; s++) {
+    const uint8_t* base = ring + slot * G::SLOT;
+    const int u = KG * s + kg;
     lr_half(base, 0);
-    if (R - (s - nst) * XLR > 16) lr_half(base, 1);
+    if (R - (u - nst) * XLR > 16) lr_half(base, 1);
     publish(IC8<0>{});
-    if (s + NS < total) static_for<G::LOADS>([&](auto ic) { load_any(ic, s + NS, lds0 + (uint32_t)slot * G::SLOT); });
+    if (s + NS < gtotal) static_for<G::LOADS>([&](auto ic) { load_any(ic, KG * (s + NS) + kg, lds0 + (uint32_t)slot * G::SLOT); });
     slot = slot + 1 == NS ? 0 : slot + 1;
   }
+  if (KG > 1 && gtotal < (total + KG - 1) / KG) publish(IC8<0>{});   // (as many barriers in every group)
   wait_vm<0>();   // zeros of stages past the end must not land in the epilogue's LDS
   __syncthreads();
+  if constexpr (KG == 2) {
+    float* sums = (float*)(mxlds + G::STG) + (wave * (MT * NT * 16)) * 64 + lane;
+    if (kg == 1) {
+#pragma unroll
+      for (int i = 0; i < MT; i++)
+#pragma unroll
+        for (int j = 0; j < NT; j++)
+#pragma unroll
+          for (int e = 0; e < 16; e++) sums[((i * NT + j) * 16 + e) * 64] = acc[i][j][e];
+    }
+    __syncthreads();
+    if (kg == 1) return;
+#pragma unroll
+    for (int i = 0; i < MT; i++)
+#pragma unroll
+      for (int j = 0; j < NT; j++)
+#pragma unroll
+        for (int e = 0; e < 16; e++) acc[i][j][e] += sums[((i * NT + j) * 16 + e) * 64];
+  }
 
   // ---------------- epilogue: 32 rows x 64 columns at a time through the wave's own LDS
   // Eight lanes hold 64 columns of a row, eight each, so that every global
@@ -529,24 +568,26 @@ hipError_t launch_gemm_mx8_t(bool bwd, int tm, const MxArgs& a, int act, hipStre
   const int tn = tm > 128 ? 256 : 128;
   const int tiles_m = (a.M + tm - 1) / tm, tiles_n = (NO + tn - 1) / tn;
   const unsigned grid = (unsigned)(((long)tiles_m * tiles_n + 7) / 8 * 8);
-#define FT_MX(BW, TM_, TN_, ACT_)                                                                              \
+#define FT_MX(BW, TM_, TN_, KG_, ACT_)                                                                              \
   do {                                                                                                              \
-    using G = MxGeom<TM_, TN_>;                                                                                \
-    const size_t lds = std::max((size_t)G::NS * G::SLOT + mx_slab(TN_, nst), (size_t)G::STG);                       \
-    k_gemm_mx8<BW, TM_, TN_, ACT_, F32><<<grid, 256, lds, st>>>(                                          \
+    using G = MxGeom<TM_, TN_>;                                                                                     \
+    const size_t sums = KG_ == 1 ? 0 : (size_t)TM_ * TN_ * 4;                                                       \
+    const size_t lds = std::max((size_t)KG_ * G::NS * G::SLOT + mx_slab(TN_, nst), (size_t)G::STG + sums);          \
+    k_gemm_mx8<BW, TM_, TN_, KG_, ACT_, F32><<<grid, 256 * KG_, lds, st>>>(                                         \
         a.x, a.xs, a.wq, a.ws, a.M, a.N, a.K, a.P, a.R, a.lr, a.bias, a.z, a.res, a.out, tiles_m, tiles_n);         \
   } while (0)
-#define FT_MX_ACT(BW, TM_, TN_)                                   \
+#define FT_MX_ACT(BW, TM_, TN_, KG_)                                   \
   do {                                                                 \
-    if (act == ACT_GELU) FT_MX(BW, TM_, TN_, ACT_GELU);           \
-    else if (act == ACT_SILU) FT_MX(BW, TM_, TN_, ACT_SILU);      \
-    else if (act == ACT_RELU) FT_MX(BW, TM_, TN_, ACT_RELU);      \
-    else FT_MX(BW, TM_, TN_, ACT_NONE);                           \
+    if (act == ACT_GELU) FT_MX(BW, TM_, TN_, KG_, ACT_GELU);           \
+    else if (act == ACT_SILU) FT_MX(BW, TM_, TN_, KG_, ACT_SILU);      \
+    else if (act == ACT_RELU) FT_MX(BW, TM_, TN_, KG_, ACT_RELU);      \
+    else FT_MX(BW, TM_, TN_, KG_, ACT_NONE);                           \
   } while (0)
-  if (tm == 256) { if (!bwd) FT_MX_ACT(false, 256, 256); else FT_MX_ACT(true, 256, 256); }
-  else if (tm == 192) { if (!bwd) FT_MX_ACT(false, 192, 256); else FT_MX_ACT(true, 192, 256); }
-  else if (tm == 128) { if (!bwd) FT_MX_ACT(false, 128, 128); else FT_MX_ACT(true, 128, 128); }
-  else { if (!bwd) FT_MX_ACT(false, 64, 128); else FT_MX_ACT(true, 64, 128); }
+  if (tm == 256) { if (!bwd) FT_MX_ACT(false, 256, 256, 1); else FT_MX_ACT(true, 256, 256, 1); }
+  else if (tm == 192) { if (!bwd) FT_MX_ACT(false, 192, 256, 1); else FT_MX_ACT(true, 192, 256, 1); }
+  else if (tm == 128) { if (!bwd) FT_MX_ACT(false, 128, 128, 1); else FT_MX_ACT(true, 128, 128, 1); }
+  else if (tiles_m * tiles_n > 256) { if (!bwd) FT_MX_ACT(false, 64, 128, 1); else FT_MX_ACT(true, 64, 128, 1); }
+  else { if (!bwd) FT_MX_ACT(false, 64, 128, 2); else FT_MX_ACT(true, 64, 128, 2); }
 #undef FT_MX_ACT
 #undef FT_MX
   return hipGetLastError();

@@ -14,18 +14,18 @@ bool gemm_mx8_supported(bool bwd, int M, int N, int K, int R) {
 // workgroups (one a CU on the wide tiles, two on the others, whose last round
 // may be of one) of a fixed part, the tile's start and end, and one per stage.
 // Measured and estimated, M x K -> N, 256x256 / 192x256 / 128x128 / 64x128:
-//   4608 x 4096 -> 16384   238 / 233 / 263 / 329    232 / 220 / 275 / 341
-//   4608 x 16384 -> 4096   306 / 247 / 260 / 300    323 / 252 / 278 / 295
-//   18432 x 4096 -> 16384  882 / 943 / 1074 / 1313  835 / 883 / 1100 / 1370
-//   2048 x 4096 -> 4096    44 / 36 / 33 / 43        46 / 37 / 31 / 38
-//   512 x 4096 -> 4096     40 / 32 / 18 / 14        46 / 37 / 17 / 13
+//   4608 x 4096 -> 16384   238 / 233 / 263 / 329    232 / 220 / 275 / 360
+//   4608 x 16384 -> 4096   306 / 247 / 260 / 300    323 / 252 / 274 / 298
+//   18432 x 4096 -> 16384  882 / 943 / 1074 / 1313  835 / 883 / 1100 / 1440
+//   2048 x 4096 -> 4096    44 / 36 / 33 / 42        46 / 37 / 31 / 40
+//   512 x 4096 -> 4096     40 / 32 / 18 / 13        46 / 37 / 17 / 11
 int gemm_mx8_tile(bool bwd, int M, int N, int K) {
   const long NO = bwd ? K : N, nst = ((bwd ? N : K) + 127) / 128;
   const struct { int tm, tn, cap; double fix, stage, fix1, stage1; size_t slot; } t[] = {
       {256, 256, 256, 8.0, 1.2, 8.0, 1.2, MxGeom<256, 256>::SLOT},
       {192, 256, 256, 7.0, 0.93, 7.0, 0.93, MxGeom<192, 256>::SLOT},
-      {128, 128, 512, 4.0, 0.83, 4.0, 0.42, 0},
-      {64, 128, 512, 4.0, 0.47, 4.0, 0.27, 0}};
+      {128, 128, 512, 4.0, 0.83, 5.0, 0.38, 0},
+      {64, 128, 512, 4.0, 0.5, 5.5, 0.16, 0}};
   int best = 64;
   double least = 1e30;
   for (const auto& g : t) {

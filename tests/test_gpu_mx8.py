@@ -278,7 +278,8 @@ def linear_case(M, K, N, R, act, residual, bias, back, f32, seed):
 
 # every kernel, with rows, columns and reductions that end inside a tile and one past it
 SIZES = [(65, 32, 32, 0), (130, 96, 160, 16), (333, 672, 1056, 48), (520, 160, 544, 128), (100, 2080, 96, 32),
-         (257, 128, 512, 0), (700, 1056, 288, 96), (64, 512, 256, 16), (1, 416, 64, 32), (256, 16384, 256, 16)]
+         (257, 128, 512, 0), (1100, 224, 2080, 80),   # more than 256 of the smallest tiles
+         (700, 1056, 288, 96), (64, 512, 256, 16), (1, 416, 64, 32), (256, 16384, 256, 16)]
 
 
 @pytest.fixture
@@ -350,7 +351,7 @@ def exact_operand(g, M, K):
 @pytest.mark.parametrize("back", [False, True])
 @pytest.mark.parametrize("tile", [1, 64, 128, 192, 256])
 @pytest.mark.parametrize("M,K,N", [(1, 32, 32), (64, 4096, 96), (37, 160, 288), (63, 96, 544), (300, 1056, 416),
-                                   (513, 2080, 1056), (1000, 4096, 256)])
+                                   (513, 2080, 1056), (1000, 4096, 256), (1030, 608, 2080)])
 def test_linear_exact(M, K, N, tile, back, on_tile):
     """Where every sum is exact in fp32, every bit is right: each element meets its block's scales and nothing else."""
     if tile == 1 and (back or M > 64):
