@@ -66,7 +66,7 @@ __device__ __forceinline__ v16f mfma_w4x8(v4i w, v8i x, v16f c, int sw, int sx) 
   return __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(a, x, c, 4, 0, SA, sw, SB, sx);
 }
 
-// a / b for 0 <= a < 2^31, b > 0: the quotient of the fp32 values is off by at
+// a / b for 0 <= a < 2^30, b > 0: the quotient of the fp32 values is off by at
 // most 2^-22 of itself; the remainder says by how much.  (A dozen instructions,
 // where the compiler's division takes three dozen, in front of everything else.)
 __device__ __forceinline__ int div_small(int a, int b) {

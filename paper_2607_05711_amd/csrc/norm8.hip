@@ -152,29 +152,47 @@ __global__ __launch_bounds__(256) void k_rmsnorm_bwd(const uint16_t* dy, const u
       for (int e = 0; e < 8; e++) acc[c][e] = 0.f;
     }
   }
-  int turn = 0;
-  for (int r0 = blockIdx.x * RPI; r0 < rows; r0 += gridDim.x * RPI, turn ^= 1) {
+  // The next row's loads go out before this row's sum (up to 4096 columns: wider
+  // rows leave no registers for it).
+  constexpr bool AHEAD = NC <= 2;
+  struct Row { v4i h[NC], g[NC], e[NC]; float r; };
+  auto load = [&](int r0, Row& d) {
     const int row = r0 + wave / WPR;
-    const bool ok = row < rows;                      // WPR == 4: always
+    const bool ok = row < rows;                      // WPR == 4: whole workgroups
     const size_t base = (size_t)row * K;
-    v4i hv[NC], gv[NC], ev[NC];
-    float s = 0.f;
-    const float r = ok ? rstd[row] : 0.f;
+    d.r = ok ? rstd[row] : 0.f;
 #pragma unroll
     for (int c = 0; c < NC; c++) {
       const int col = (c * LPR + lr) * 8;
-      hv[c] = gv[c] = ev[c] = v4i{0, 0, 0, 0};
+      d.h[c] = d.g[c] = d.e[c] = v4i{0, 0, 0, 0};
       if (ok && col < K) {
-        hv[c] = *(const v4i*)(h + base + col);
-        gv[c] = *(const v4i*)(dy + base + col);
-        if (dh) ev[c] = *(const v4i*)(dh + base + col);
+        d.h[c] = *(const v4i*)(h + base + col);
+        d.g[c] = *(const v4i*)(dy + base + col);
+        if (dh) d.e[c] = *(const v4i*)(dh + base + col);
       }
     }
+  };
+  int turn = 0;
+  Row next;
+  if constexpr (AHEAD) load(blockIdx.x * RPI, next);
+  for (int r0 = blockIdx.x * RPI; r0 < rows; r0 += gridDim.x * RPI, turn ^= 1) {
+    const int row = r0 + wave / WPR;
+    const bool ok = row < rows;
+    const size_t base = (size_t)row * K;
+    Row cur;
+    if constexpr (AHEAD) {
+      cur = next;
+      load(r0 + gridDim.x * RPI, next);
+    } else {
+      load(r0, cur);
+    }
+    const float r = cur.r;
+    float s = 0.f;
 #pragma unroll
     for (int c = 0; c < NC; c++) {
       float a[8], g[8], ww[8];
-      unpack_bf16x8(hv[c], a);
-      unpack_bf16x8(gv[c], g);
+      unpack_bf16x8(cur.h[c], a);
+      unpack_bf16x8(cur.g[c], g);
       unpack_bf16x8(wv[c], ww);
 #pragma unroll
       for (int e = 0; e < 8; e++) {
@@ -194,10 +212,10 @@ __global__ __launch_bounds__(256) void k_rmsnorm_bwd(const uint16_t* dy, const u
     for (int c = 0; c < NC; c++) {
       const int col = (c * LPR + lr) * 8;
       float a[8], g[8], ww[8], d[8];
-      unpack_bf16x8(hv[c], a);
-      unpack_bf16x8(gv[c], g);
+      unpack_bf16x8(cur.h[c], a);
+      unpack_bf16x8(cur.g[c], g);
       unpack_bf16x8(wv[c], ww);
-      unpack_bf16x8(ev[c], d);
+      unpack_bf16x8(cur.e[c], d);
 #pragma unroll
       for (int e = 0; e < 8; e++) d[e] = fmaf(r, fmaf(-(a[e] * r), m, g[e] * ww[e]), d[e]);
       if (ok && col < K) *(v4i*)(dx + base + col) = pack_bf16x8(d);

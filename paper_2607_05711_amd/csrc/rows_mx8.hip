@@ -1,5 +1,5 @@
 // The 8-bit linear's forward over few rows (decoding), gfx950:
-//   out[M, N] = act(X W^T + P U + bias) + residual,  M <= 64
+//   out[M, N] = act(X W^T + P U + bias) + residual,  M <= 32
 // the product of gemm_mx8.hip where the weight's bytes are all that counts.
 //
 // A workgroup of 8 waves takes 16 to 64 columns (rows of W) and all rows of X; a
@@ -40,7 +40,7 @@ __global__ __launch_bounds__(64 * RW) void k_rows_mx8(const uint8_t* __restrict_
                                                       int M, int N, int K, const float* __restrict__ P, int R,
                                                       const uint16_t* __restrict__ U, const uint16_t* __restrict__ bias,
                                                       int act, uint16_t* z, const void* res, void* out, int out_f32) {
-  constexpr int RSTEPS = MT * NT <= 2 ? 4 : 2;          // steps whose loads are in flight together
+  constexpr int RSTEPS = MT == 1 || MT * NT <= 2 ? 4 : 2;   // steps whose loads are in flight together
   constexpr int WN = 16 * NT;                           // columns of the workgroup
   __shared__ float sums[RW][MT * 16][WN + 1];
   const int tid = threadIdx.x, lane = tid & 63, l16 = lane & 15, g = lane >> 4;
@@ -142,15 +142,15 @@ __global__ __launch_bounds__(64 * RW) void k_rows_mx8(const uint8_t* __restrict_
 }
 
 // Against the tile kernel (64 x 128 tiles), us a call, M x K -> N: 16 x 4096 -> 16384
-// 11 against 14, 16 x 16384 -> 4096 14 against 39, 33 x 4096 -> 4096 11 against 13;
-// but every workgroup reads X, in rows of 128 bytes a step: 64 x 4096 -> 4096 16
-// against 13, 64 x 4096 -> 16384 24 against 14.
-bool rows_mx8_better(int M, int N, int K) { return M <= 16 || (M <= 32 && N <= 8192) || (M <= 48 && N <= 4096); }
+// 10.6 against 12.4, 16 x 16384 -> 4096 14 against 29, 32 x 4096 -> 4096 9.4 against
+// 11.3; but every workgroup reads X, in rows of 128 bytes a step: 64 x 4096 -> 4096
+// took 16 against 11.
+bool rows_mx8_better(int M, int N, int K) { return M <= 16 || (M <= kRowsMx8Max && N <= 8192); }
 
 hipError_t launch_rows_mx8(const MxArgs& a, int act, bool out_f32, hipStream_t st) {
   // Columns a workgroup: 16 while that makes no more workgroups than CUs, then
   // 32 and 64, which read X half and a quarter as often (X is read by every one).
-  const int wgs = a.N / 16, nt = wgs <= 256 ? 1 : wgs <= 512 || a.M > 32 ? 2 : 4;
+  const int wgs = a.N / 16, nt = wgs <= 256 ? 1 : wgs <= 512 ? 2 : 4;
 #define FT_ROWS8(MT_, NT_)                                                                                      \
   k_rows_mx8<MT_, NT_><<<(a.N + 16 * NT_ - 1) / (16 * NT_), 64 * RW, 0, st>>>(                                  \
       a.x, a.xs, a.wq, a.ws, a.M, a.N, a.K, a.P, a.R, a.lr, a.bias, act, a.z, a.res, a.out, out_f32 ? 1 : 0)
@@ -161,9 +161,7 @@ hipError_t launch_rows_mx8(const MxArgs& a, int act, bool out_f32, hipStream_t s
     else FT_ROWS8(MT_, 4);              \
   } while (0)
   if (a.M <= 16) FT_ROWS8_NT(1);
-  else if (a.M <= 32) FT_ROWS8_NT(2);
-  else if (nt == 1) FT_ROWS8(4, 1);
-  else FT_ROWS8(4, 2);
+  else FT_ROWS8_NT(2);
 #undef FT_ROWS8_NT
 #undef FT_ROWS8
   return hipGetLastError();

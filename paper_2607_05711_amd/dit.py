@@ -13,7 +13,9 @@ embeddings, joint attention and gated residuals run on kernels of their own
 (_dit_ops).  AdamW updates
 the LoRA factors (fp32 masters; the library reads their bf16 copies).
 
-The same model with 16-bit LoRA linears (bf16 weights and adapters as torch
+The same model on 8-bit activations and gradients (kind "fp8": the same frozen
+MXFP4 weights, E4M3 operands with one scale per 32) is the layer's more exact
+and slower form.  The same model with 16-bit LoRA linears (bf16 weights and adapters as torch
 matmuls) is the paper's BF16 LoRA baseline.
 
 Weights are random (timing does not depend on values); inputs are seeded
@@ -77,6 +79,59 @@ class _TripleBranchFn(torch.autograd.Function):
         return dx, dA, dB, None
 
 
+class _TripleBranch8Fn(torch.autograd.Function):
+    """_TripleBranchFn on MXFP8 activations and gradients."""
+
+    @staticmethod
+    def forward(ctx, x, A, B, layer):
+        x = x.contiguous()
+        xq, xs, P, _ = _lib.ft_quantize8(x, proj=layer.D)
+        y = _lib.ft_linear8_fwd(xq, xs, layer.wq, layer.ws, P, layer.U, layer.bias)
+        ctx.save_for_backward(x, P)
+        ctx.layer = layer
+        return y
+
+    @staticmethod
+    def backward(ctx, dy):
+        x, P = ctx.saved_tensors
+        L = ctx.layer
+        dy = dy.contiguous()
+        gq, gs, Qp, _ = _lib.ft_quantize8(dy, proj=L.U, proj_layout=_lib.FT_PROJ_R_BY_COLS)
+        dx = _lib.ft_linear8_bwd_input(gq, gs, L.wq, L.ws, Qp, L.D) if ctx.needs_input_grad[0] else None
+        dA, dB = _lib.ft_lora_grads(x, dy, P, Qp, L.r, col0=L.rs)
+        return dx, dA, dB, None
+
+
+class _MlpPair8Fn(torch.autograd.Function):
+    """_MlpPairFn on MXFP8 activations and gradients: the GELU in FC1's epilogue, its derivative in that of FC2's input
+    gradient."""
+
+    @staticmethod
+    def forward(ctx, x, A1, B1, A2, B2, fc1, fc2):
+        x = x.contiguous()
+        xq, xs, P1, _ = _lib.ft_quantize8(x, proj=fc1.D)
+        h, z = _lib.ft_linear8_fwd(xq, xs, fc1.wq, fc1.ws, P1, fc1.U, fc1.bias, act=_lib.FT_ACT_GELU, want_z=True)
+        hq, hs, P2, _ = _lib.ft_quantize8(h, proj=fc2.D)
+        y = _lib.ft_linear8_fwd(hq, hs, fc2.wq, fc2.ws, P2, fc2.U, fc2.bias)
+        ctx.save_for_backward(x, P1, z, h, P2)
+        ctx.fc = (fc1, fc2)
+        return y
+
+    @staticmethod
+    def backward(ctx, dy):
+        x, P1, z, h, P2 = ctx.saved_tensors
+        fc1, fc2 = ctx.fc
+        dy = dy.contiguous()
+        by_r = _lib.FT_PROJ_R_BY_COLS
+        gq, gs, Qp2, _ = _lib.ft_quantize8(dy, proj=fc2.U, proj_layout=by_r)
+        dz = _lib.ft_linear8_bwd_input(gq, gs, fc2.wq, fc2.ws, Qp2, fc2.D, z=z, act=_lib.FT_ACT_GELU)
+        dzq, dzs, Qp1, _ = _lib.ft_quantize8(dz, proj=fc1.U, proj_layout=by_r)
+        dx = _lib.ft_linear8_bwd_input(dzq, dzs, fc1.wq, fc1.ws, Qp1, fc1.D) if ctx.needs_input_grad[0] else None
+        dA2, dB2 = _lib.ft_lora_grads(h, dy, P2, Qp2, fc2.r, col0=fc2.rs)
+        dA1, dB1 = _lib.ft_lora_grads(x, dz, P1, Qp1, fc1.r, col0=fc1.rs)
+        return dx, dA1, dB1, dA2, dB2, None, None
+
+
 class _MlpPairFn(torch.autograd.Function):
     """FC1 -> GELU(tanh) -> FC2 with the fused calls (MLP fusion)."""
 
@@ -137,6 +192,15 @@ class FourTuneLinear(torch.nn.Module):
         return y.reshape(*shape[:-1], self.N)
 
 
+class FourTuneLinear8(FourTuneLinear):
+    """FourTuneLinear whose activations and gradients are MXFP8 (the weight, factors and bias are the same)."""
+
+    def forward(self, x):
+        shape = x.shape
+        y = _TripleBranch8Fn.apply(x.reshape(-1, self.K), self.A, self.B, self)
+        return y.reshape(*shape[:-1], self.N)
+
+
 class FourTuneMLP(torch.nn.Module):
     """MLP pair D -> F -> D (GELU tanh) of two triple-branch linears, forward
     and backward through the fused calls."""
@@ -154,6 +218,25 @@ class FourTuneMLP(torch.nn.Module):
         f1, f2 = self.fc1, self.fc2
         shape = x.shape
         y = _MlpPairFn.apply(x.reshape(-1, f1.K), f1.A, f1.B, f2.A, f2.B, f1, f2)
+        return y.reshape(*shape[:-1], f2.N)
+
+
+class FourTuneMLP8(torch.nn.Module):
+    """FourTuneMLP on MXFP8 activations and gradients."""
+
+    def __init__(self, Dm, Fm, r, rs, gen, device):
+        super().__init__()
+        self.fc1 = FourTuneLinear8(Dm, Fm, r, rs, gen, device)
+        self.fc2 = FourTuneLinear8(Fm, Dm, r, rs, gen, device)
+
+    def sync(self):
+        self.fc1.sync()
+        self.fc2.sync()
+
+    def forward(self, x):
+        f1, f2 = self.fc1, self.fc2
+        shape = x.shape
+        y = _MlpPair8Fn.apply(x.reshape(-1, f1.K), f1.A, f1.B, f2.A, f2.B, f1, f2)
         return y.reshape(*shape[:-1], f2.N)
 
 
@@ -273,6 +356,8 @@ class DiT(torch.nn.Module):
         gen.manual_seed(seed)
         if kind == "fp4":
             make_linear, make_mlp = FourTuneLinear, FourTuneMLP
+        elif kind == "fp8":
+            make_linear, make_mlp = FourTuneLinear8, FourTuneMLP8
         elif kind == "bf16":
             make_linear, make_mlp = Bf16LoraLinear, Bf16LoraMLP
         else:
