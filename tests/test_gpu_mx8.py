@@ -356,6 +356,8 @@ def test_linear_exact(M, K, N, tile, back, on_tile):
     """Where every sum is exact in fp32, every bit is right: each element meets its block's scales and nothing else."""
     if tile == 1 and (back or M > 32):
         pytest.skip("the kernel of few rows: forward, up to 32")
+    if (N if back else K) > 4096:
+        pytest.skip("sums of more than 4096 products pass 24 bits")
     on_tile(tile)
     g = ref.gen(M + K + N)
     wq = torch.randint(0, 256, (N, K // 2), dtype=U8, device=DEV, generator=g)
