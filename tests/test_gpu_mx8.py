@@ -318,6 +318,36 @@ def test_linear(M, K, N, R, act, residual, f32, back, tile, on_tile):
     linear_case(M, K, N, R, act, residual, R != 48, back, f32, M + K + N + act)
 
 
+@pytest.mark.parametrize("tile", [192, 256])
+@pytest.mark.parametrize("back", [False, True])
+@pytest.mark.parametrize("M,K,N,R,act,residual,f32", [
+    (4400, 544, 4352, 48, 2, True, False), (4400, 512, 4352, 0, 0, False, True), (9000, 640, 2208, 16, 1, False, False),
+    (2500, 2080, 8224, 128, 0, True, False), (13000, 384, 2080, 0, 3, True, False), (26000, 512, 1056, 0, 0, False, False)])
+def test_linear_many_wide_tiles(M, K, N, R, act, residual, f32, back, tile, on_tile):
+    """More wide tiles than CUs, with ragged last rows and columns among them."""
+    if back:
+        K, N = N, K
+    on_tile(tile)
+    linear_case(M, K, N, R, act, residual, R != 48, back, f32, M + K)
+
+
+@pytest.mark.parametrize("tile", [192, 256])
+@pytest.mark.parametrize("back", [False, True])
+def test_linear_exact_many_wide_tiles(tile, back, on_tile):
+    on_tile(tile)
+    M, K, N = (7000, 512, 4352) if not back else (7000, 4352, 512)
+    g = ref.gen(tile)
+    wq = torch.randint(0, 256, (N, K // 2), dtype=U8, device=DEV, generator=g)
+    ws = torch.randint(126, 128, (N // 32, K // 32), device=DEV, generator=g).to(U8)
+    xq, xs = exact_operand(g, M, N if back else K)
+    X, W = ref.values8(xq, xs), ref.values4(wq, ws)
+    want = X @ (W if back else W.T)
+    f = L.ft_linear8_bwd_input if back else L.ft_linear8_fwd
+    assert torch.equal(f(xq, xs, wq, ws, out_dtype=F32).double(), want)
+    for _ in range(3):
+        assert torch.equal(f(xq, xs, wq, ws), want.float().to(BF))
+
+
 @pytest.mark.parametrize("M,K,N", [(4608, 1024, 4096), (1111, 2080, 3168), (300, 4096, 1024), (65, 65536, 32)])
 @pytest.mark.parametrize("back", [False, True])
 def test_linear_by_rule(M, K, N, back):
