@@ -4,10 +4,12 @@
 
 namespace ft {
 
-// 32-bit offsets of the weight, a tile and the scales; the weight's scales in LDS.
+// 32-bit offsets of the weight, a tile and the scales; the weight's scales in
+// LDS; a tile count that 32 bits hold.
 bool gemm_mx8_supported(bool bwd, int M, int N, int K, int R) {
   const long NO = bwd ? K : N, KR = bwd ? N : K, lim = 1l << 31;
-  return (long)N * K / 2 < lim && KR <= 65536 && NO <= 1 << 20 && (KR + 127) / 128 * 4 * M < lim && NO * std::max(R, 1) * 2 < lim;
+  return (long)N * K / 2 < lim && KR <= 65536 && NO <= 1 << 20 && (KR + 127) / 128 * 4 * M < lim &&
+         NO * std::max(R, 1) * 2 < lim && M * NO <= 1l << 40;
 }
 
 // Which tile: the one of the least estimated time, in microseconds: rounds of

@@ -495,6 +495,84 @@ def test_rows_past_the_last_stay():
         assert bool((buf[M:] == 7).all()) and bool((codes[M:] == 7).all())
 
 
+def test_offsets_past_32_bits():
+    """More than 2^31 elements: the last rows are those of a short call on them."""
+    g = ref.gen(40)
+    M, K, m = 530_000, 4096, 70                               # 2.17e9
+    x = torch.empty((M, K), dtype=BF, device=DEV)
+    x[-m:] = ref.normal(g, m, K)
+    x[:-m] = 1
+    w, p = ref.normal(g, K), ref.normal(g, K, 16)
+    tail = x[-m:].clone()
+    h, y, c, s, r = L.ft_rmsnorm_quantize8(x, w, x, h=x, want_y=True, want_rstd=True)       # h in x's place
+    h2, y2, c2, s2, r2 = L.ft_rmsnorm_quantize8(tail, w, tail, want_y=True, want_rstd=True)
+    for a, b in ((h, h2), (y, y2), (c.view(U8), c2.view(U8)), (r, r2)):
+        assert torch.equal(a[-m:], b)
+    assert torch.equal(s[:, -m:], s2)
+    dx, dw = L.ft_rmsnorm_bwd(y, h, w, r, dx=y)                                             # dx in dy's place
+    dx2, _ = L.ft_rmsnorm_bwd(y2, h2, w, r2)
+    assert torch.equal(dx[-m:], dx2) and bool(dw.isfinite().all())
+    for proj in (None, p):
+        c, s, P, _ = L.ft_quantize8(h, proj=proj, codes=c, scales=s)
+        c2, s2, P2, _ = L.ft_quantize8(h2, proj=proj)
+        assert torch.equal(c[-m:].view(U8), c2.view(U8)) and torch.equal(s[:, -m:], s2)
+        if proj is not None:                                  # (its sums may run over other pieces)
+            near(P[-m:], P2, (h2.double().abs() @ p.double().abs()) * 2 * (K + 16) * 2.0 ** -24)
+    del h, y, dx, x
+    q, qs = exact_operand(g, m, K)
+    c[-m:], s[:, -m:] = q, qs
+    wq = torch.randint(0, 256, (64, K // 2), dtype=U8, device=DEV, generator=g)
+    ws = torch.full((2, K // 32), 127, dtype=U8, device=DEV)
+    want = ref.values8(q, qs) @ ref.values4(wq, ws).T
+    assert torch.equal(L.ft_linear8_fwd(c, s, wq, ws, out_dtype=F32)[-m:].double(), want)
+    wq = torch.randint(0, 256, (K, 32), dtype=U8, device=DEV, generator=g)
+    ws = torch.full((K // 32, 2), 127, dtype=U8, device=DEV)
+    want = ref.values8(q, qs) @ ref.values4(wq, ws)
+    assert torch.equal(L.ft_linear8_bwd_input(c, s, wq, ws, out_dtype=F32)[-m:].double(), want)
+
+
+def test_long_outputs_past_32_bits():
+    """More than 2^31 outputs, on whatever tile the sizes take: the last rows against 64 bits."""
+    g = ref.gen(41)
+    M, K, N, m = 140_000, 64, 16384, 300                      # 2.3e9
+    xq, xs = exact_operand(g, M, K)
+    wq = torch.randint(0, 256, (N, K // 2), dtype=U8, device=DEV, generator=g)
+    ws = torch.full((N // 32, K // 32), 127, dtype=U8, device=DEV)
+    y = torch.ones((M, N), dtype=BF, device=DEV)
+    L.ft_linear8_fwd(xq, xs, wq, ws, residual=y, y=y)
+    want = ref.values8(xq[-m:], xs[:, -m:].contiguous()) @ ref.values4(wq, ws).T + 1
+    assert torch.equal(y[-m:], want.float().to(BF))
+    assert torch.equal(y[:5], (ref.values8(xq[:5], xs[:, :5].contiguous()) @ ref.values4(wq, ws).T + 1).float().to(BF))
+
+
+def test_refusals_of_gpu_tensors():
+    """Layouts that the kernels do not hold are refused before a launch."""
+    g = ref.gen(42)
+    x, w = ref.normal(g, 8, 256), ref.normal(g, 256)
+    wq, ws = ref.weight(g, 64, 256)
+    q, s, _, _ = L.ft_quantize8(x)
+    odd = ref.normal(g, 8 * 256 + 1)[1:].view(8, 256)         # 2 bytes past an allocation's start
+    for call in (lambda: L.ft_quantize8(odd), lambda: L.ft_rmsnorm_quantize8(odd, w),
+                 lambda: L.ft_linear8_fwd(q, s, wq, ws, residual=ref.normal(g, 8 * 64 + 1)[1:].view(8, 64)),
+                 lambda: L.ft_quantize8(x, act=L.FT_ACT_SILU), lambda: L.ft_linear8_fwd(q, s, wq, ws, act=7),
+                 lambda: L.ft_linear8_bwd_input(L.ft_quantize8(x[:, :64].contiguous())[0],
+                                               L.ft_quantize8(x[:, :64].contiguous())[1], wq, ws, act=L.FT_ACT_GELU)):
+        with pytest.raises(L.FourTuneError):
+            call()
+    for call in (lambda: L.ft_quantize8(x.t()), lambda: L.ft_quantize8(x[:, ::2]), lambda: L.ft_rmsnorm_quantize8(x, w[:128]),
+                 lambda: L.ft_rmsnorm_quantize8(x, w, h=x), lambda: L.ft_quantize8(x, v=x),
+                 lambda: L.ft_linear8_fwd(q, s[:1], wq, ws), lambda: L.ft_linear8_fwd(q, s.transpose(0, 1), wq, ws),
+                 lambda: L.ft_linear8_fwd(q[:, :128].contiguous(), s, wq, ws), lambda: L.ft_linear8_fwd(q, s, wq, ws[:1].contiguous()),
+                 lambda: L.ft_linear8_fwd(q, s, wq, ws, y=torch.empty((8, 64), dtype=torch.float16, device=DEV)),
+                 lambda: L.ft_linear8_fwd(q, s, wq, ws, bias=w), lambda: L.ft_rmsnorm_bwd(x, x, w, w)):
+        with pytest.raises((ValueError, TypeError)):
+            call()
+    with pytest.raises(TypeError):
+        L.ft_linear8_fwd(q, s, wq, ws, P=torch.zeros((8, 16), device=DEV))
+    with pytest.raises(TypeError):
+        L.ft_linear8_fwd(q, s, wq, ws, residual=torch.zeros((8, 64), device=DEV))      # another type than y's
+
+
 # ------------------------------------------------------- together, as they run
 class Block:
     """A feed-forward block of the residual stream: norm, wide layer, activation, narrow layer, added to the stream;

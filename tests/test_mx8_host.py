@@ -84,6 +84,7 @@ def test_linear_refusals(back):
     assert f(**{i: 65536 + 32}) == f(**{"K" if back else "N": (1 << 20) + 32}) == _lib.FT_ERR_UNSUPPORTED
     assert f(N=65536, K=65536) == _lib.FT_ERR_UNSUPPORTED               # N K / 2 = 2 GiB
     assert f(M=1 << 25, **{i: 2048}) == _lib.FT_ERR_UNSUPPORTED         # 2 GiB of scales
+    assert f(M=(1 << 22) + 1, **{i: 32, "K" if back else "N": 1 << 20}) == _lib.FT_ERR_UNSUPPORTED
     assert f(M=0) == f(**{"K" if back else "N": 0}) == _lib.FT_OK
 
 
