@@ -348,7 +348,8 @@ ft_status ft_linear_bwd_input_nvfp4(const uint8_t *gq, const uint8_t *gs, const 
  *
  * The weight is ft_quantize_blockwise's (block_rows = 32), and so are D, U and
  * the adapter gradients: ft_lora_grads takes these calls' P, Qp and bf16
- * tensors unchanged.
+ * tensors unchanged.  Outputs and workspaces overlap no other argument but where
+ * a declaration says so.
  */
 typedef enum ft_act { FT_ACT_NONE = 0, FT_ACT_GELU = 1, FT_ACT_SILU = 2, FT_ACT_RELU = 3 } ft_act;
 
@@ -368,7 +369,8 @@ typedef enum ft_act { FT_ACT_NONE = 0, FT_ACT_GELU = 1, FT_ACT_SILU = 2, FT_ACT_
  *   codes, scales  MXFP8 of y, or both NULL.  y or codes is required.
  *   rstd         fp32 [rows] or NULL (kept for ft_rmsnorm_bwd).
  * cols % 32 == 0, cols <= 16384 (FT_ERR_UNSUPPORTED above); eps >= 0.
- * rows == 0 is a no-op.
+ * rows == 0 is a no-op.  Squares are summed in fp32: a row whose sum passes
+ * 2^128 (|h| from 2^57 on at the widest) gives rstd = 0 and y = 0.
  */
 ft_status ft_rmsnorm_quantize8(const void *x, const void *residual, const void *w, int64_t rows, int64_t cols,
                                float eps, void *h, void *y, uint8_t *codes, uint8_t *scales, float *rstd,

@@ -10,6 +10,10 @@
 // directions are bound by HBM.  A 32-element block lies in a lane quad, whose
 // maximum takes two DPP steps; a row of 16 lanes makes the four scale bytes of
 // 128 columns, which are one dword of the scales' [K / 128, M, 4].
+//
+// 4608 x 4096 with residual and every output moves 170 MB in 37 us, its gradients
+// with dh and dw 151 MB in 34 us: 4.6 and 4.4 TB/s where a 2 GiB copy reaches
+// 5.0.  One row takes 2.7 us.
 #include "ft_device.h"
 #include "ft_kernels.h"
 

@@ -9,6 +9,8 @@
 // lane, so that all of the workgroup's loads are in flight together and every
 // access is a run of 512 bytes or more of a row.  The scale dwords (four
 // blocks, 128 columns) of 16 rows meet in LDS and leave as runs of 64 bytes.
+// 1111 x 11264 through SiLU' moves 88 MB in 16.9 us, 5.2 TB/s (a 2 GiB copy: 5.0;
+// some of this fits the last-level cache).
 #include "ft_device.h"
 #include "ft_kernels.h"
 

@@ -631,7 +631,7 @@ hipError_t launch_quant_gelu(const uint16_t* z, int rows, int cols, uint16_t* h,
                              const uint16_t* proj, int R, float* proj_out, float* ws, int max_groups, int max_chain,
                              hipStream_t st) {
   if (R > 0)
-    return launch_quant_proj(z, rows, cols, codes, scales, proj, R, 0, false, proj_out, ws, max_groups, max_chain, h, st);
+    return launch_quant_proj(z, rows, cols, codes, scales, proj, R, 0, 0, proj_out, ws, max_groups, max_chain, h, st);
   dim3 grid((rows + 127) / 128, (cols + 383) / 384);
   k_quant_rows<1, 0, 4, 384, 0, false, true><<<grid, 256, 0, st>>>(z, rows, cols, codes, scales, nullptr, 0, nullptr,
                                                                   nullptr, SrKey{}, 1, h);

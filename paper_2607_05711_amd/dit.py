@@ -15,8 +15,8 @@ the LoRA factors (fp32 masters; the library reads their bf16 copies).
 
 The same model on 8-bit activations and gradients (kind "fp8": the same frozen
 MXFP4 weights, E4M3 operands with one scale per 32) is the layer's more exact
-and slower form.  The same model with 16-bit LoRA linears (bf16 weights and adapters as torch
-matmuls) is the paper's BF16 LoRA baseline.
+and slower form.  The same model with 16-bit LoRA linears (bf16 weights and
+adapters as torch matmuls) is the paper's BF16 LoRA baseline.
 
 Weights are random (timing does not depend on values); inputs are seeded
 synthetic tensors with FLUX.1-dev's shapes at 1024x1024 (4096 image + 512
@@ -193,7 +193,10 @@ class FourTuneLinear(torch.nn.Module):
 
 
 class FourTuneLinear8(FourTuneLinear):
-    """FourTuneLinear whose activations and gradients are MXFP8 (the weight, factors and bias are the same)."""
+    """FourTuneLinear whose activations and gradients are MXFP8 (the weight, factors and bias are the same).
+
+    A step is captured into a HIP graph after its warm-up's results are gone: torch's autograd keeps the stream of the
+    first live backward graph of a parameter."""
 
     def forward(self, x):
         shape = x.shape
