@@ -398,9 +398,9 @@ ft_status ft_rmsnorm_quantize8(const void* x, const void* residual, const void* 
   FT_TRY(check_dim("cols", cols, 32));
   if (cols > kNormCols) return fail(FT_ERR_UNSUPPORTED, "cols = %lld: at most %lld", (long long)cols, (long long)kNormCols);
   if (!(eps >= 0.0f)) return fail(FT_ERR_UNSUPPORTED, "eps = %g", (double)eps);
+  if (rows == 0 || cols == 0) return FT_OK;            // (empty tensors may have no address)
   if (!residual != !h) return fail(FT_ERR_UNSUPPORTED, "h goes with a residual");
   if (!codes != !scales) return fail(FT_ERR_NULL, "codes and scales go together");
-  if (rows == 0 || cols == 0) return FT_OK;
   if (!x || !w || (!y && !codes)) return fail(FT_ERR_NULL, "x, w, and y or codes are required");
   if (!aligned16(x) || !aligned16(residual) || !aligned16(w) || !aligned16(h) || !aligned16(y) || !aligned16(codes) ||
       !aligned16(scales) || !aligned16(rstd))
@@ -444,10 +444,10 @@ ft_status ft_quantize8(const void* src, const void* z, ft_act act, int64_t rows,
   FT_TRY(check_dim("cols", cols, 32));
   if (cols > (1 << 20)) return fail(FT_ERR_UNSUPPORTED, "cols = %lld: at most 2^20", (long long)cols);
   FT_TRY(check_act(act));
-  if (!z != (act == FT_ACT_NONE) || (!z && v)) return fail(FT_ERR_UNSUPPORTED, "z goes with an activation, and v with z");
   if (proj_layout != FT_PROJ_COLS_BY_R && proj_layout != FT_PROJ_R_BY_COLS)
     return fail(FT_ERR_UNSUPPORTED, "proj_layout = %d", (int)proj_layout);
-  if (rows == 0 || cols == 0) return FT_OK;
+  if (rows == 0 || cols == 0) return FT_OK;            // (empty tensors may have no address)
+  if (!z != (act == FT_ACT_NONE) || (!z && v)) return fail(FT_ERR_UNSUPPORTED, "z goes with an activation, and v with z");
   if (!src || !codes || !scales) return fail(FT_ERR_NULL, "src, codes and scales are required");
   if (!aligned16(src) || !aligned16(z) || !aligned16(v) || !aligned16(codes) || !aligned16(scales))
     return fail(FT_ERR_ALIGN, "src, z, v, codes and scales must be 16-byte aligned");
@@ -473,8 +473,8 @@ static ft_status linear8(bool bwd, int tile, const uint8_t* x, const uint8_t* xs
   FT_TRY(check_dim("K", K, 32));
   if (dtype != FT_BF16 && dtype != FT_F32) return fail(FT_ERR_UNSUPPORTED, "output dtype = %d", (int)dtype);
   FT_TRY(check_act(act));
+  if (M == 0 || (bwd ? K : N) == 0) return FT_OK;      // (empty tensors may have no address)
   if (bwd && !z != (act == FT_ACT_NONE)) return fail(FT_ERR_UNSUPPORTED, "z goes with an activation");
-  if (M == 0 || (bwd ? K : N) == 0) return FT_OK;
   if ((bwd ? N : K) == 0) return fail(FT_ERR_SHAPE, "empty reduction");
   if (!x || !xs || !wq || !ws || !out) return fail(FT_ERR_NULL, "codes, scales and the output are required");
   if (!aligned16(x) || !aligned16(xs) || !aligned16(wq) || !aligned16(ws) || !aligned16(out) || !aligned16(bias) ||

@@ -144,3 +144,11 @@ def test_reference_norm_gradients_against_differences():
             plus, minus = ((t + s * 1e-5 * u) for s in (1, -1))
             diff = (f(plus, w) - f(minus, w)) / 2e-5 if t is h else (f(h, plus) - f(h, minus)) / 2e-5
             assert abs(diff - float((d * u).sum())) < 1e-6 * (1 + abs(diff))
+
+
+def test_no_rows_with_an_activation():
+    """Empty tensors have no address: no rows is a no-op whatever goes with them."""
+    L = _lib.load()
+    assert L.ft_quantize8(None, None, _lib.FT_ACT_GELU, 0, 64, None, None, None, None, 0, 0, None, None, 0, None) == _lib.FT_OK
+    assert L.ft_linear8_bwd_input(None, None, 0, 64, None, None, 32, None, 0, None, None, _lib.FT_ACT_SILU, None, None,
+                                  _lib.FT_BF16, None) == _lib.FT_OK
