@@ -433,8 +433,8 @@ size_t ft_quantize8_workspace_size(int64_t rows, int64_t cols, int32_t R, ft_pro
  *   residual [M, N] of y's type, or NULL; it may be y itself.
  *   z        bf16 [M, N] or NULL: saved for ft_quantize8 or ft_linear8_bwd_input.
  *   y        [M, N], bf16 or fp32.
- * FT_ERR_UNSUPPORTED: K > 65536, N > 2^20, M N > 2^40, N K / 2, R N * 2, or
- * M K / 32 from 2 GiB on.
+ * FT_ERR_UNSUPPORTED: K > 65536, N > 2^20, M N from 2^39 on, N K / 2,
+ * R N * 2, or M K / 32 from 2 GiB on.
  */
 ft_status ft_linear8_fwd(const uint8_t *xq, const uint8_t *xs, int64_t M, int64_t K, const uint8_t *wq,
                          const uint8_t *ws, int64_t N, const float *P, int32_t R, const void *U, const void *bias,
@@ -450,8 +450,8 @@ ft_status ft_linear8_fwd(const uint8_t *xq, const uint8_t *xs, int64_t M, int64_
  *   z, act   bf16 [M, K] and its activation, or NULL and FT_ACT_NONE.
  *   residual [M, K] of dx's type, or NULL; it may be dx itself.
  *   dx       [M, K], bf16 or fp32.
- * FT_ERR_UNSUPPORTED: N > 65536, K > 2^20, M K > 2^40, N K / 2, R K * 2, or
- * M N / 32 from 2 GiB on.
+ * FT_ERR_UNSUPPORTED: N > 65536, K > 2^20, M K from 2^39 on, N K / 2,
+ * R K * 2, or M N / 32 from 2 GiB on.
  */
 ft_status ft_linear8_bwd_input(const uint8_t *gq, const uint8_t *gs, int64_t M, int64_t N, const uint8_t *wq,
                                const uint8_t *ws, int64_t K, const float *Qp, int32_t R, const void *D, const void *z,

@@ -92,6 +92,13 @@ bool gemm_fp4_fused_supported(bool bwd, int M, int N, int K, int R, int R2);
 int gemm_fp4_col_tiles(int NO);
 
 // ---- 8-bit activations and gradients (MXFP8: E4M3, scales [cols / 128, rows, 4])
+// A launch's threads along one dimension wrap at 2^32 without an error (the
+// workgroups past it never run), so that kernels with a workgroup for every few
+// rows spread them over two dimensions: workgroup blockIdx.x + kGridX * (the other).
+constexpr unsigned kGridX = 1u << 20;
+struct RowGrid { unsigned x, other; };
+inline RowGrid row_grid(unsigned n) { return n <= kGridX ? RowGrid{n, 1} : RowGrid{kGridX, (n + kGridX - 1) / kGridX}; }
+
 // h = bf16(x + res) (res NULL: h is x and nothing is stored); y = h / rms(h) * w;
 // y, codes and scales, rstd: NULL for none.  K <= 16384, a multiple of 32.
 hipError_t launch_rmsnorm_q8(const uint16_t* x, const uint16_t* res, const uint16_t* w, float eps, int rows, int K,

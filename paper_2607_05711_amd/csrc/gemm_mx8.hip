@@ -5,11 +5,14 @@
 namespace ft {
 
 // 32-bit offsets of the weight, a tile and the scales; the weight's scales in
-// LDS; a tile count that 32 bits hold.
+// LDS; fewer than 2^24 workgroups of 256 threads (see row_grid): 2^39 outputs are
+// 1.4 * 2^23 tiles of 192x256, and the rule takes smaller ones only for outputs of
+// up to 128 columns, whose rows end below 2^29, and for reductions whose weight
+// leaves them fewer than 2^16 columns by 2^20 rows.
 bool gemm_mx8_supported(bool bwd, int M, int N, int K, int R) {
   const long NO = bwd ? K : N, KR = bwd ? N : K, lim = 1l << 31;
   return (long)N * K / 2 < lim && KR <= 65536 && NO <= 1 << 20 && (KR + 127) / 128 * 4 * M < lim &&
-         NO * std::max(R, 1) * 2 < lim && M * NO <= 1l << 40;
+         NO * std::max(R, 1) * 2 < lim && M * NO < 1l << 39;
 }
 
 // Which tile: the one of the least estimated time, in microseconds: rounds of

@@ -39,7 +39,7 @@ __global__ __launch_bounds__(256) void k_rmsnorm_q8(const uint16_t* x, const uin
   constexpr int LPR = 64 * WPR;
   __shared__ float part[4];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, lr = threadIdx.x % LPR;
-  const int nwg = WPR == 4 ? rows : (rows + 3) / 4, block = xcd_order(blockIdx.x, nwg);
+  const int nwg = WPR == 4 ? rows : (rows + 3) / 4, block = xcd_order(blockIdx.x + kGridX * blockIdx.y, nwg);
   if (block >= nwg) return;                          // the whole workgroup
   const int row = block * (4 / WPR) + wave / WPR;
   if (WPR == 1 && row >= rows) return;
@@ -118,7 +118,8 @@ hipError_t launch_rmsnorm_q8(const uint16_t* x, const uint16_t* res, const uint1
   const bool wide = K > 2048 || rows < 4096;
   const int nc = (K + (wide ? 2047 : 511)) / (wide ? 2048 : 512);
   const int nwg = (wide ? rows : (rows + 3) / 4);
-  const unsigned grid = (unsigned)((nwg + 7) / 8 * 8);
+  const RowGrid rg = row_grid((unsigned)((nwg + 7) / 8 * 8));
+  const dim3 grid(rg.x, rg.other);
 #define FT_NORM(NC_, WPR_) \
   k_rmsnorm_q8<NC_, WPR_><<<grid, 256, 0, st>>>(x, res, w, eps, rows, K, h, y, codes, (uint32_t*)scales, rstd)
   if (wide) {

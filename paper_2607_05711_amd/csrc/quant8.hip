@@ -25,7 +25,7 @@ __global__ __launch_bounds__(256) void k_quant8(const uint16_t* src, const uint1
                                                 uint16_t* v, uint8_t* __restrict__ codes, uint32_t* __restrict__ scales) {
   __shared__ uint32_t sc[4][Q8_ROWS];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const int row0 = blockIdx.x * Q8_ROWS, col = blockIdx.y * Q8_COLS + lane * 8;
+  const int row0 = (blockIdx.x + kGridX * blockIdx.z) * Q8_ROWS, col = blockIdx.y * Q8_COLS + lane * 8;
   constexpr int T = Q8_ROWS / 4;
   v4i x[T], zv[T];
 #pragma unroll
@@ -66,7 +66,8 @@ __global__ __launch_bounds__(256) void k_quant8(const uint16_t* src, const uint1
 
 hipError_t launch_quant8(const uint16_t* src, const uint16_t* z, int act, int rows, int cols, uint16_t* v, uint8_t* codes,
                          uint8_t* scales, hipStream_t st) {
-  const dim3 grid((rows + Q8_ROWS - 1) / Q8_ROWS, (cols + Q8_COLS - 1) / Q8_COLS);
+  const RowGrid rg = row_grid((unsigned)(rows + Q8_ROWS - 1) / Q8_ROWS);
+  const dim3 grid(rg.x, (cols + Q8_COLS - 1) / Q8_COLS, rg.other);
 #define FT_Q8(ACT_, Z_) k_quant8<ACT_, Z_><<<grid, 256, 0, st>>>(src, z, rows, cols, v, codes, (uint32_t*)scales)
   if (!z) FT_Q8(ACT_NONE, false);
   else if (act == ACT_GELU) FT_Q8(ACT_GELU, true);

@@ -1,0 +1,47 @@
+"""The 8-bit operators at the ends of what their documentation allows."""
+import pytest
+import torch
+
+from tests import _mx8 as ref
+from tests._mx8 import BF, U8
+from paper_2607_05711_amd import _lib as L
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda:0"
+
+
+def some_rows(g, M, K, runs):
+    """Ones, with random values in the runs of rows that are looked at."""
+    x = torch.ones((M, K), dtype=BF, device=DEV)
+    for a, b in runs:
+        x[a:b] = ref.normal(g, b - a, K)
+    return x
+
+
+@pytest.mark.parametrize("M,K", [((1 << 26) + 41, 32), ((1 << 24) + 19, 2080)])
+def test_norm_of_more_rows_than_a_launch_dimension_holds(M, K):
+    """A workgroup each, or one for four: 2^32 threads and more.  Every run of rows is that of a short call on it."""
+    torch.cuda.empty_cache()
+    g = ref.gen(K)
+    runs = [(0, 70), (M // 2 - 35, M // 2 + 35), ((1 << 22) - 35, (1 << 22) + 35), ((1 << 20) - 35, (1 << 20) + 35), (M - 70, M)]
+    x, w = some_rows(g, M, K, runs), ref.normal(g, K)
+    _, _, c, s, r = L.ft_rmsnorm_quantize8(x, w, want_rstd=True)
+    for a, b in runs:
+        _, _, c2, s2, r2 = L.ft_rmsnorm_quantize8(x[a:b].clone(), w, want_rstd=True)
+        assert torch.equal(c[a:b].view(U8), c2.view(U8)) and torch.equal(s[:, a:b], s2) and torch.equal(r[a:b], r2)
+    del x, c, s, r
+    torch.cuda.empty_cache()
+
+
+def test_quantize_of_more_rows_than_a_launch_dimension_holds():
+    torch.cuda.empty_cache()
+    M, K = (1 << 28) + 5, 32
+    g = ref.gen(1)
+    runs = [(0, 70), ((1 << 24) - 35, (1 << 24) + 35), (M // 2 - 35, M // 2 + 35), (M - 70, M)]
+    x = some_rows(g, M, K, runs)
+    c, s, _, _ = L.ft_quantize8(x)
+    for a, b in runs:
+        c2, s2 = ref.mxfp8(x[a:b])
+        assert torch.equal(c[a:b].view(U8), c2) and torch.equal(s[:, a:b], s2)
+    del x, c, s
+    torch.cuda.empty_cache()

@@ -152,3 +152,16 @@ def test_no_rows_with_an_activation():
     assert L.ft_quantize8(None, None, _lib.FT_ACT_GELU, 0, 64, None, None, None, None, 0, 0, None, None, 0, None) == _lib.FT_OK
     assert L.ft_linear8_bwd_input(None, None, 0, 64, None, None, 32, None, 0, None, None, _lib.FT_ACT_SILU, None, None,
                                   _lib.FT_BF16, None) == _lib.FT_OK
+
+
+@built
+@pytest.mark.parametrize("back", [False, True])
+def test_more_outputs_than_a_launch_holds(back):
+    """2^39 outputs, four times what the card's memory holds: past 2^24 workgroups a launch would run some of them only."""
+    L = _lib.load()
+    for M, o in ((1 << 20, 1 << 20), (1 << 19, 1 << 20), (1 << 28, 1 << 11)):
+        if back:
+            s = L.ft_linear8_bwd_input(A, A, M, 32, A, A, o, N0, 0, N0, N0, 0, N0, A, 0, N0)
+        else:
+            s = L.ft_linear8_fwd(A, A, M, 32, A, A, o, N0, 0, N0, N0, 0, N0, N0, A, 0, N0)
+        assert s == _lib.FT_ERR_UNSUPPORTED
