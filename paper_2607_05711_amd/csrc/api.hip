@@ -485,7 +485,7 @@ static ft_status linear8(bool bwd, int tile, const uint8_t* x, const uint8_t* xs
     return fail(FT_ERR_UNSUPPORTED, "M = %lld, N = %lld, K = %lld: operands too large for 32-bit offsets", (long long)M,
                 (long long)N, (long long)K);
   if (tile == 0)
-    tile = !bwd && ft::rows_mx8_better((int)M, (int)N, (int)K) ? 1 : ft::gemm_mx8_tile(bwd, (int)M, (int)N, (int)K);
+    tile = !bwd && ft::rows_mx8_better((int)M, (int)N) ? 1 : ft::gemm_mx8_tile(bwd, (int)M, (int)N, (int)K);
   const ft::MxArgs a{x, xs, wq, ws, (int)M, (int)N, (int)K, P, R, (const uint16_t*)lr, (const uint16_t*)bias, (uint16_t*)z,
                      residual, out};
   if (tile == 1) return hip_status(ft::launch_rows_mx8(a, (int)act, dtype == FT_F32, stream), "linear8 fwd (few rows)");
@@ -513,7 +513,7 @@ int ftx_gemm_kernel(int bwd, int64_t M, int64_t N, int64_t K, int32_t R, int out
 }
 // What a call of the 8-bit linear runs on, and the call on a kernel of the tests' choosing.
 int ftx_linear8_tile(int bwd, int64_t M, int64_t N, int64_t K) {
-  return !bwd && ft::rows_mx8_better((int)M, (int)N, (int)K) ? 1 : ft::gemm_mx8_tile(bwd != 0, (int)M, (int)N, (int)K);
+  return !bwd && ft::rows_mx8_better((int)M, (int)N) ? 1 : ft::gemm_mx8_tile(bwd != 0, (int)M, (int)N, (int)K);
 }
 ft_status ftx_linear8_fwd(int tile, const uint8_t* xq, const uint8_t* xs, int64_t M, int64_t K, const uint8_t* wq,
                           const uint8_t* ws, int64_t N, const float* P, int32_t R, const void* U, const void* bias,

@@ -137,7 +137,7 @@ hipError_t launch_gemm_mx8_f32(bool bwd, int tile, const MxArgs& a, int act, hip
 
 // The forward over few rows (M <= kRowsMx8Max), and whether it is the faster one there.
 constexpr int kRowsMx8Max = 32;
-bool rows_mx8_better(int M, int N, int K);
+bool rows_mx8_better(int M, int N);
 hipError_t launch_rows_mx8(const MxArgs& a, int act, bool out_f32, hipStream_t st);
 
 // Adapter gradients; token chunks leave partials in ws (lora_grads_workspace bytes).

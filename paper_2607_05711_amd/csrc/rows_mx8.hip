@@ -149,24 +149,24 @@ __global__ __launch_bounds__(64 * RW) void k_rows_mx8(const uint8_t* __restrict_
 // 10.6 against 12.4, 16 x 16384 -> 4096 14 against 29, 32 x 4096 -> 4096 9.4 against
 // 11.3; but every workgroup reads X, in rows of 128 bytes a step: 64 x 4096 -> 4096
 // took 16 against 11.
-bool rows_mx8_better(int M, int N, int K) { return M <= 16 || (M <= kRowsMx8Max && N <= 8192); }
+bool rows_mx8_better(int M, int N) { return M <= 16 || (M <= kRowsMx8Max && N <= 8192); }
 
 hipError_t launch_rows_mx8(const MxArgs& a, int act, bool out_f32, hipStream_t st) {
   // Columns a workgroup: 16 while that makes no more workgroups than CUs, then
-  // 32 and 64, which read X half and a quarter as often (X is read by every one).
+  // 32 and, up to 16 rows, 64, which read X half and a quarter as often (X is read
+  // by every one).  More rows come with at most 8192 columns (rows_mx8_better).
   const int wgs = a.N / 16, nt = wgs <= 256 ? 1 : wgs <= 512 ? 2 : 4;
 #define FT_ROWS8(MT_, NT_)                                                                                      \
   k_rows_mx8<MT_, NT_><<<(a.N + 16 * NT_ - 1) / (16 * NT_), 64 * RW, 0, st>>>(                                  \
       a.x, a.xs, a.wq, a.ws, a.M, a.N, a.K, a.P, a.R, a.lr, a.bias, act, a.z, a.res, a.out, out_f32 ? 1 : 0)
-#define FT_ROWS8_NT(MT_)                \
-  do {                                  \
-    if (nt == 1) FT_ROWS8(MT_, 1);      \
-    else if (nt == 2) FT_ROWS8(MT_, 2); \
-    else FT_ROWS8(MT_, 4);              \
-  } while (0)
-  if (a.M <= 16) FT_ROWS8_NT(1);
-  else FT_ROWS8_NT(2);
-#undef FT_ROWS8_NT
+  if (a.M <= 16) {
+    if (nt == 1) FT_ROWS8(1, 1);
+    else if (nt == 2) FT_ROWS8(1, 2);
+    else FT_ROWS8(1, 4);
+  } else {
+    if (nt == 1) FT_ROWS8(2, 1);
+    else FT_ROWS8(2, 2);
+  }
 #undef FT_ROWS8
   return hipGetLastError();
 }

@@ -165,3 +165,30 @@ def test_more_outputs_than_a_launch_holds(back):
         else:
             s = L.ft_linear8_fwd(A, A, M, 32, A, A, o, N0, 0, N0, N0, 0, N0, N0, A, 0, N0)
         assert s == _lib.FT_ERR_UNSUPPORTED
+
+
+@built
+def test_rows_kernel_has_no_instance_that_no_call_reaches():
+    """More than 16 rows go there with at most 8192 columns, where a workgroup takes 16 or 32 of them."""
+    names = open(_lib.LIB_PATH, "rb").read()
+    assert all(b"k_rows_mx8ILi%dELi%dE" % mn in names for mn in ((1, 1), (1, 2), (1, 4), (2, 1), (2, 2)))
+    assert b"k_rows_mx8ILi2ELi4E" not in names
+
+
+@built
+@pytest.mark.parametrize("back,M,K,N,want", [
+    # few rows: the forward's kernel for them (1), up to 16 rows, and up to 32 of at most 8192 columns
+    (False, 1, 4096, 4096, 1), (False, 16, 4096, 16384, 1), (False, 17, 4096, 8192, 1), (False, 32, 4096, 8192, 1),
+    (False, 17, 4096, 8224, 64), (False, 32, 4096, 16384, 64), (False, 33, 4096, 4096, 64), (True, 1, 4096, 4096, 64),
+    # the sizes whose times on all four tiles stand at the rule
+    (False, 4608, 4096, 16384, 192), (False, 4608, 16384, 4096, 192), (False, 18432, 4096, 16384, 256),
+    (False, 2048, 4096, 4096, 128), (False, 512, 4096, 4096, 64), (True, 4608, 4096, 16384, 192),
+    # 416 stages are the most whose weight scales fit beside the ring of a 256x256 tile; past them two rounds of
+    # 128x128 tiles (4 + 0.83 us a stage) come before two of 192x256 (7 + 0.93)
+    (False, 16384, 53248, 1024, 256), (False, 16384, 53280, 1024, 128), (True, 16384, 1024, 53248, 256),
+    (True, 16384, 1024, 53280, 128),
+])
+def test_kernel_of_a_product(back, M, K, N, want):
+    f = _lib.load().ftx_linear8_tile
+    f.argtypes, f.restype = [ctypes.c_int] + [ctypes.c_int64] * 3, ctypes.c_int
+    assert f(int(back), M, N, K) == want
