@@ -79,12 +79,30 @@ class _TripleBranchFn(torch.autograd.Function):
         return dx, dA, dB, None
 
 
+class _First(torch.autograd.Function):
+    """g, a gradient that depends on the tensors `of` and has no derivative of its own: refused where one is asked for."""
+
+    @staticmethod
+    def forward(ctx, g, *of):
+        return g.clone()
+
+    @staticmethod
+    def backward(ctx, *_):
+        raise RuntimeError("the 8-bit layers' gradients cannot be differentiated: they have first derivatives only")
+
+
+def _first(grads, *of):
+    """Gradients as a backward returns them; under create_graph they refuse a second derivative, which would lack their part."""
+    if not torch.is_grad_enabled():
+        return grads
+    return tuple(g if g is None else _First.apply(g, *of) for g in grads)
+
+
 class _TripleBranch8Fn(torch.autograd.Function):
-    """_TripleBranchFn on MXFP8 activations and gradients."""
+    """_TripleBranchFn on MXFP8 activations and gradients; x contiguous."""
 
     @staticmethod
     def forward(ctx, x, A, B, layer):
-        x = x.contiguous()
         xq, xs, P, _ = _lib.ft_quantize8(x, proj=layer.D)
         y = _lib.ft_linear8_fwd(xq, xs, layer.wq, layer.ws, P, layer.U, layer.bias)
         ctx.save_for_backward(x, P)
@@ -94,21 +112,20 @@ class _TripleBranch8Fn(torch.autograd.Function):
     @staticmethod
     def backward(ctx, dy):
         x, P = ctx.saved_tensors
-        L = ctx.layer
+        L, of = ctx.layer, (dy, x, ctx.layer.A, ctx.layer.B)
         dy = dy.contiguous()
         gq, gs, Qp, _ = _lib.ft_quantize8(dy, proj=L.U, proj_layout=_lib.FT_PROJ_R_BY_COLS)
         dx = _lib.ft_linear8_bwd_input(gq, gs, L.wq, L.ws, Qp, L.D) if ctx.needs_input_grad[0] else None
         dA, dB = _lib.ft_lora_grads(x, dy, P, Qp, L.r, col0=L.rs)
-        return dx, dA, dB, None
+        return _first((dx, dA, dB), *of) + (None,)
 
 
 class _MlpPair8Fn(torch.autograd.Function):
     """_MlpPairFn on MXFP8 activations and gradients: the GELU in FC1's epilogue, its derivative in that of FC2's input
-    gradient."""
+    gradient; x contiguous."""
 
     @staticmethod
     def forward(ctx, x, A1, B1, A2, B2, fc1, fc2):
-        x = x.contiguous()
         xq, xs, P1, _ = _lib.ft_quantize8(x, proj=fc1.D)
         h, z = _lib.ft_linear8_fwd(xq, xs, fc1.wq, fc1.ws, P1, fc1.U, fc1.bias, act=_lib.FT_ACT_GELU, want_z=True)
         hq, hs, P2, _ = _lib.ft_quantize8(h, proj=fc2.D)
@@ -121,6 +138,7 @@ class _MlpPair8Fn(torch.autograd.Function):
     def backward(ctx, dy):
         x, P1, z, h, P2 = ctx.saved_tensors
         fc1, fc2 = ctx.fc
+        of = (dy, x, fc1.A, fc1.B, fc2.A, fc2.B)
         dy = dy.contiguous()
         by_r = _lib.FT_PROJ_R_BY_COLS
         gq, gs, Qp2, _ = _lib.ft_quantize8(dy, proj=fc2.U, proj_layout=by_r)
@@ -129,7 +147,7 @@ class _MlpPair8Fn(torch.autograd.Function):
         dx = _lib.ft_linear8_bwd_input(dzq, dzs, fc1.wq, fc1.ws, Qp1, fc1.D) if ctx.needs_input_grad[0] else None
         dA2, dB2 = _lib.ft_lora_grads(h, dy, P2, Qp2, fc2.r, col0=fc2.rs)
         dA1, dB1 = _lib.ft_lora_grads(x, dz, P1, Qp1, fc1.r, col0=fc1.rs)
-        return dx, dA1, dB1, dA2, dB2, None, None
+        return _first((dx, dA1, dB1, dA2, dB2), *of) + (None, None)
 
 
 class _MlpPairFn(torch.autograd.Function):
@@ -200,7 +218,7 @@ class FourTuneLinear8(FourTuneLinear):
 
     def forward(self, x):
         shape = x.shape
-        y = _TripleBranch8Fn.apply(x.reshape(-1, self.K), self.A, self.B, self)
+        y = _TripleBranch8Fn.apply(x.reshape(-1, self.K).contiguous(), self.A, self.B, self)
         return y.reshape(*shape[:-1], self.N)
 
 
@@ -239,7 +257,7 @@ class FourTuneMLP8(torch.nn.Module):
     def forward(self, x):
         f1, f2 = self.fc1, self.fc2
         shape = x.shape
-        y = _MlpPair8Fn.apply(x.reshape(-1, f1.K), f1.A, f1.B, f2.A, f2.B, f1, f2)
+        y = _MlpPair8Fn.apply(x.reshape(-1, f1.K).contiguous(), f1.A, f1.B, f2.A, f2.B, f1, f2)
         return y.reshape(*shape[:-1], f2.N)
 
 
