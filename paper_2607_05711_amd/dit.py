@@ -105,17 +105,17 @@ class _TripleBranch8Fn(torch.autograd.Function):
     def forward(ctx, x, A, B, layer):
         xq, xs, P, _ = _lib.ft_quantize8(x, proj=layer.D)
         y = _lib.ft_linear8_fwd(xq, xs, layer.wq, layer.ws, P, layer.U, layer.bias)
-        ctx.save_for_backward(x, P)
+        ctx.save_for_backward(x, P, layer.D, layer.U)   # (saved: a sync() before the backward is noticed)
         ctx.layer = layer
         return y
 
     @staticmethod
     def backward(ctx, dy):
-        x, P = ctx.saved_tensors
+        x, P, D, U = ctx.saved_tensors
         L, of = ctx.layer, (dy, x, ctx.layer.A, ctx.layer.B)
         dy = dy.contiguous()
-        gq, gs, Qp, _ = _lib.ft_quantize8(dy, proj=L.U, proj_layout=_lib.FT_PROJ_R_BY_COLS)
-        dx = _lib.ft_linear8_bwd_input(gq, gs, L.wq, L.ws, Qp, L.D) if ctx.needs_input_grad[0] else None
+        gq, gs, Qp, _ = _lib.ft_quantize8(dy, proj=U, proj_layout=_lib.FT_PROJ_R_BY_COLS)
+        dx = _lib.ft_linear8_bwd_input(gq, gs, L.wq, L.ws, Qp, D) if ctx.needs_input_grad[0] else None
         dA, dB = _lib.ft_lora_grads(x, dy, P, Qp, L.r, col0=L.rs)
         return _first((dx, dA, dB), *of) + (None,)
 
@@ -130,21 +130,21 @@ class _MlpPair8Fn(torch.autograd.Function):
         h, z = _lib.ft_linear8_fwd(xq, xs, fc1.wq, fc1.ws, P1, fc1.U, fc1.bias, act=_lib.FT_ACT_GELU, want_z=True)
         hq, hs, P2, _ = _lib.ft_quantize8(h, proj=fc2.D)
         y = _lib.ft_linear8_fwd(hq, hs, fc2.wq, fc2.ws, P2, fc2.U, fc2.bias)
-        ctx.save_for_backward(x, P1, z, h, P2)
+        ctx.save_for_backward(x, P1, z, h, P2, fc1.D, fc1.U, fc2.D, fc2.U)
         ctx.fc = (fc1, fc2)
         return y
 
     @staticmethod
     def backward(ctx, dy):
-        x, P1, z, h, P2 = ctx.saved_tensors
+        x, P1, z, h, P2, D1, U1, D2, U2 = ctx.saved_tensors
         fc1, fc2 = ctx.fc
         of = (dy, x, fc1.A, fc1.B, fc2.A, fc2.B)
         dy = dy.contiguous()
         by_r = _lib.FT_PROJ_R_BY_COLS
-        gq, gs, Qp2, _ = _lib.ft_quantize8(dy, proj=fc2.U, proj_layout=by_r)
-        dz = _lib.ft_linear8_bwd_input(gq, gs, fc2.wq, fc2.ws, Qp2, fc2.D, z=z, act=_lib.FT_ACT_GELU)
-        dzq, dzs, Qp1, _ = _lib.ft_quantize8(dz, proj=fc1.U, proj_layout=by_r)
-        dx = _lib.ft_linear8_bwd_input(dzq, dzs, fc1.wq, fc1.ws, Qp1, fc1.D) if ctx.needs_input_grad[0] else None
+        gq, gs, Qp2, _ = _lib.ft_quantize8(dy, proj=U2, proj_layout=by_r)
+        dz = _lib.ft_linear8_bwd_input(gq, gs, fc2.wq, fc2.ws, Qp2, D2, z=z, act=_lib.FT_ACT_GELU)
+        dzq, dzs, Qp1, _ = _lib.ft_quantize8(dz, proj=U1, proj_layout=by_r)
+        dx = _lib.ft_linear8_bwd_input(dzq, dzs, fc1.wq, fc1.ws, Qp1, D1) if ctx.needs_input_grad[0] else None
         dA2, dB2 = _lib.ft_lora_grads(h, dy, P2, Qp2, fc2.r, col0=fc2.rs)
         dA1, dB1 = _lib.ft_lora_grads(x, dz, P1, Qp1, fc1.r, col0=fc1.rs)
         return _first((dx, dA1, dB1, dA2, dB2), *of) + (None, None)

@@ -74,3 +74,18 @@ def test_first_derivatives_under_create_graph(layer):
         assert all(torch.equal(a, b) for a, b in zip(got, want))
         with pytest.raises(RuntimeError, match="first derivatives only"):
             got[0].float().sum().backward()
+
+
+def test_factors_changed_before_the_backward(layer):
+    """Gradients are those of the factors that the forward used: refreshed ones in between are refused."""
+    x = data()
+    y = layer(x)
+    with torch.no_grad():
+        for p in layer.parameters():
+            p.mul_(2.0)
+    layer.sync()
+    with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+        y.float().sum().backward()
+    y = layer(x)                                              # and a new forward takes the new ones
+    y.float().sum().backward()
+    assert all(p.grad is not None for p in layer.parameters())
