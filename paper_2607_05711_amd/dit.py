@@ -23,6 +23,7 @@ synthetic tensors with FLUX.1-dev's shapes at 1024x1024 (4096 image + 512
 text tokens, hidden 3072, 24 heads of 128, MLP 12288, 19 double and 38 single
 blocks).
 """
+import weakref
 from dataclasses import dataclass
 
 import torch
@@ -98,6 +99,38 @@ def _first(grads, *of):
     return tuple(g if g is None else _First.apply(g, *of) for g in grads)
 
 
+def _on_default_stream(device):
+    return device.type == "cuda" and _lib._stream(device) == 0
+
+
+#: Layer -> [its live backward graphs, whether the first of them was made on the default stream].
+_graphs = weakref.WeakKeyDictionary()
+
+
+def _noted(y, *layers):
+    """y, an output of these layers, whose backward graph is noted in them.
+
+    torch keeps the accumulation of a parameter's gradient on the stream of the first live graph that reaches it.  A
+    backward captured meanwhile would wait for that stream and draw it into the capture, which ends the process where
+    it is the default one."""
+    node = y.grad_fn
+    if node is not None:
+        for layer in layers:
+            g = _graphs.setdefault(layer, [weakref.WeakSet(), False])
+            if not g[0]:
+                g[1] = _on_default_stream(layer.A.device)
+            if layer.A.requires_grad or layer.B.requires_grad:
+                g[0].add(node)
+    return y
+
+
+def _not_drawn_in(*layers):
+    if any(_graphs[layer][1] for layer in layers if layer in _graphs) and torch.cuda.is_current_stream_capturing():
+        raise RuntimeError("this backward cannot be captured: the results of an eager pass on the default stream are "
+                           "alive (a loss, say), and their graph holds the parameters' gradients on that stream; drop "
+                           "them before the capture, or run such passes on another stream")
+
+
 class _TripleBranch8Fn(torch.autograd.Function):
     """_TripleBranchFn on MXFP8 activations and gradients; x contiguous."""
 
@@ -113,6 +146,7 @@ class _TripleBranch8Fn(torch.autograd.Function):
     def backward(ctx, dy):
         x, P, D, U = ctx.saved_tensors
         L, of = ctx.layer, (dy, x, ctx.layer.A, ctx.layer.B)
+        _not_drawn_in(L)
         dy = dy.contiguous()
         gq, gs, Qp, _ = _lib.ft_quantize8(dy, proj=U, proj_layout=_lib.FT_PROJ_R_BY_COLS)
         dx = _lib.ft_linear8_bwd_input(gq, gs, L.wq, L.ws, Qp, D) if ctx.needs_input_grad[0] else None
@@ -139,6 +173,7 @@ class _MlpPair8Fn(torch.autograd.Function):
         x, P1, z, h, P2, D1, U1, D2, U2 = ctx.saved_tensors
         fc1, fc2 = ctx.fc
         of = (dy, x, fc1.A, fc1.B, fc2.A, fc2.B)
+        _not_drawn_in(fc1, fc2)
         dy = dy.contiguous()
         by_r = _lib.FT_PROJ_R_BY_COLS
         gq, gs, Qp2, _ = _lib.ft_quantize8(dy, proj=U2, proj_layout=by_r)
@@ -213,12 +248,13 @@ class FourTuneLinear(torch.nn.Module):
 class FourTuneLinear8(FourTuneLinear):
     """FourTuneLinear whose activations and gradients are MXFP8 (the weight, factors and bias are the same).
 
-    A step is captured into a HIP graph after its warm-up's results are gone: torch's autograd keeps the stream of the
-    first live backward graph of a parameter."""
+    A step is captured into a HIP graph after the results of eager steps on the default stream are gone; a backward
+    captured beside them is refused.  Gradients are first derivatives, of the factors that the forward used: a sync()
+    between forward and backward is refused too."""
 
     def forward(self, x):
         shape = x.shape
-        y = _TripleBranch8Fn.apply(x.reshape(-1, self.K).contiguous(), self.A, self.B, self)
+        y = _noted(_TripleBranch8Fn.apply(x.reshape(-1, self.K).contiguous(), self.A, self.B, self), self)
         return y.reshape(*shape[:-1], self.N)
 
 
@@ -257,7 +293,7 @@ class FourTuneMLP8(torch.nn.Module):
     def forward(self, x):
         f1, f2 = self.fc1, self.fc2
         shape = x.shape
-        y = _MlpPair8Fn.apply(x.reshape(-1, f1.K).contiguous(), f1.A, f1.B, f2.A, f2.B, f1, f2)
+        y = _noted(_MlpPair8Fn.apply(x.reshape(-1, f1.K).contiguous(), f1.A, f1.B, f2.A, f2.B, f1, f2), f1, f2)
         return y.reshape(*shape[:-1], f2.N)
 
 

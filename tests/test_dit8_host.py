@@ -89,3 +89,35 @@ def test_factors_changed_before_the_backward(layer):
     y = layer(x)                                              # and a new forward takes the new ones
     y.float().sum().backward()
     assert all(p.grad is not None for p in layer.parameters())
+
+
+def test_backward_captured_beside_an_eager_graph(layer, monkeypatch):
+    """A parameter's accumulation stays on the stream of its first live graph, and the default stream cannot be captured:
+    refused before any work is sent there, and only then."""
+    now = {"default": True, "capturing": False}
+    monkeypatch.setattr(dit, "_on_default_stream", lambda device: now["default"], raising=False)
+    monkeypatch.setattr(torch.cuda, "is_current_stream_capturing", lambda: now["capturing"])
+    x, leaves = data(), tuple(layer.parameters())
+
+    def captured():
+        now.update(default=False, capturing=True)
+        try:
+            return torch.autograd.grad(layer(x).float().sum(), (x,) + leaves)
+        finally:
+            now.update(default=True, capturing=False)
+
+    held = layer(x).float().sum()                             # an eager step's loss, kept
+    with pytest.raises(RuntimeError, match="default stream"):
+        captured()
+    held.backward()                                           # its graph is of use still, and lives on
+    with pytest.raises(RuntimeError, match="default stream"):
+        captured()
+    del held
+    want = captured()
+    with torch.no_grad():
+        kept = layer(x)                                       # has no graph
+    now["default"] = False
+    beside = layer(x)                                         # an eager graph on a stream of its own
+    for a, b in zip(captured(), want):
+        assert torch.equal(a, b)
+    assert kept.shape == beside.shape

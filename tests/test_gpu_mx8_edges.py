@@ -1,10 +1,13 @@
 """The 8-bit operators at the ends of what their documentation allows."""
+import gc
+
 import pytest
 import torch
 
 from tests import _mx8 as ref
 from tests._mx8 import BF, U8
 from paper_2607_05711_amd import _lib as L
+from paper_2607_05711_amd import dit
 
 pytestmark = pytest.mark.gpu
 DEV = "cuda:0"
@@ -45,3 +48,31 @@ def test_quantize_of_more_rows_than_a_launch_dimension_holds():
         assert torch.equal(c[a:b].view(U8), c2) and torch.equal(s[:, a:b], s2)
     del x, c, s
     torch.cuda.empty_cache()
+
+
+@pytest.mark.parametrize("kind", [dit.FourTuneLinear8, dit.FourTuneMLP8])
+def test_capture_beside_the_results_of_an_eager_step(kind):
+    """Refused while a loss from the default stream lives, and captured once it is gone."""
+    g = ref.gen(3)
+    m = kind(128, 96 if kind is dit.FourTuneLinear8 else 256, 16, 16, g, DEV)
+    leaves, x = tuple(m.parameters()), ref.normal(g, 33, 128).requires_grad_(True)
+    held = m(x)
+    dy = torch.ones_like(held)
+    step = lambda: torch.autograd.grad(m(x), (x,) + leaves, dy)  # noqa: E731
+    torch.cuda.synchronize()
+    with pytest.raises(RuntimeError, match="default stream"):
+        with torch.cuda.graph(torch.cuda.CUDAGraph()):
+            step()
+    want = torch.autograd.grad(held, (x,) + leaves, dy)
+    del held
+    gc.collect()                                              # (the refusal's traceback)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        outs = step()
+    for _ in range(3):
+        for t in outs:
+            t.fill_(1)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(outs, want))
+        want = step()
