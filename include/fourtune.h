@@ -370,7 +370,8 @@ typedef enum ft_act { FT_ACT_NONE = 0, FT_ACT_GELU = 1, FT_ACT_SILU = 2, FT_ACT_
  *   rstd         fp32 [rows] or NULL (kept for ft_rmsnorm_bwd).
  * cols % 32 == 0, cols <= 16384 (FT_ERR_UNSUPPORTED above); eps >= 0.
  * rows == 0 is a no-op.  Squares are summed in fp32: a row whose sum passes
- * 2^128 (|h| from 2^57 on at the widest) gives rstd = 0 and y = 0.
+ * 2^128 (|h| from 2^57 on at the widest) gives rstd = 0 and y = 0, and with eps =
+ * 0 a row whose squares all fall below 2^-149 (|h| < 2^-75) rstd = infinity.
  */
 ft_status ft_rmsnorm_quantize8(const void *x, const void *residual, const void *w, int64_t rows, int64_t cols,
                                float eps, void *h, void *y, uint8_t *codes, uint8_t *scales, float *rstd,
@@ -420,12 +421,18 @@ size_t ft_quantize8_workspace_size(int64_t rows, int64_t cols, int32_t R, ft_pro
  * Forward of the triple-branch linear on 8-bit activations:
  *   a[m,n] = sum_k DQ(xq)[m,k] DQ(wq)[n,k] + sum_j P[m,j] U[j,n] + bias[n]
  *   z[m,n] = bf16(a[m,n]);   y[m,n] = act(a[m,n]) + residual[m,n]
- * FP8 x FP4 block-scaled MFMA, fp32 throughout, one rounding of each output.
+ * FP8 x FP4 block-scaled MFMA, sums in fp32, one rounding of each output.
  * The matrix instruction adds products in groups of eight reduction elements
- * and drops what lies below 2^-14 of the largest one's power of two: some 4e-6
- * to 3e-5 of a result in the 2-norm.  bf16 results carry that inside their
- * rounding; fp32 results come from two products (X split at |x| = 2) whose
- * groups are exact, at twice the matrix time.
+ * and drops what lies below 2^-14 of the largest one's power of two.  bf16
+ * results take that.  In the 2-norm it is 5e-6 of them on normal values and 2e-5
+ * with 0.5 % of channels x30 (their rounding is 1.7e-3, X's to E4M3 2.6e-2).
+ * Single elements whose terms nearly cancel feel it more: 0.06 % and 0.3 % of them
+ * are off by more than half a bf16 step, 2^-8, of themselves before they are
+ * rounded.  fp32 results come from two products (X split at |x| = 2) whose groups
+ * are exact, at twice the matrix time, and so do bf16 ones of up to 16 rows (32
+ * with N <= 8192): such rows are not bit for bit those of a longer call.
+ * P enters as its first 16 bits, for fp32 results as its first 24.  GELU and SiLU,
+ * on the hardware's exp2 and reciprocal, are off by at most 2^-20 (1 + |a|).
  *   xq, xs   X in MXFP8 [M, K], scales [ceil(K / 128), M, 4].
  *   wq, ws, P, R, U, bias  as in ft_linear_fwd.
  *   act      FT_ACT_NONE; FT_ACT_GELU (the tanh form); FT_ACT_SILU,

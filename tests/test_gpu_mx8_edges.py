@@ -76,3 +76,15 @@ def test_capture_beside_the_results_of_an_eager_step(kind):
         torch.cuda.synchronize()
         assert all(torch.equal(a, b) for a, b in zip(outs, want))
         want = step()
+
+
+def test_norm_of_rows_at_the_ends_of_fp32():
+    """Squares past 2^128 and below 2^-149, without an eps and with one."""
+    x = torch.ones((4, 64), dtype=BF, device=DEV)
+    x[0], x[1], x[2] = 2.0 ** 64, 2.0 ** -76, 2.0 ** -70
+    w = torch.ones(64, dtype=BF, device=DEV)
+    _, y, _, _, r = L.ft_rmsnorm_quantize8(x, w, eps=0.0, want_y=True, want_rstd=True)
+    assert r.tolist() == [0.0, torch.inf, 2.0 ** 70, 1.0]     # 2^-140, a subnormal, is held exactly
+    assert bool((y[0] == 0).all()) and bool(y[1].isinf().all()) and bool((y[2:] == 1).all())
+    _, y, _, _, r = L.ft_rmsnorm_quantize8(x, w, eps=2.0 ** -20, want_y=True, want_rstd=True)
+    assert bool((r[1:3] == 1024).all()) and bool((y[1] == 2.0 ** -66).all())
