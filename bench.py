@@ -63,7 +63,7 @@ def parse():
     ap.add_argument("--numerics", action="store_true",
                     help="time the quantizer's numerics variants at the QKV shapes, print one JSON line, exit")
     ap.add_argument("--dit", action="store_true",
-                    help="time one synthetic FLUX DiT training step, W4A4G4 against BF16 LoRA; print one JSON line")
+                    help="time one synthetic FLUX DiT training step, W4A4G4 and W4A8G8 against BF16 LoRA; print one JSON line")
     ap.add_argument("--stability", action="store_true",
                     help="run the synthetic gradient-norm stability probe, print one JSON line, exit")
     ap.add_argument("--no-clock-sample", action="store_true",
@@ -711,15 +711,16 @@ def library_gemm(torch, _lib, dev, seed, steps=20, warmup=5):
     return out
 
 
-def dit_step_timing(torch, dev, seed, steps, warmup, cfg=None):
+def dit_step_timing(torch, dev, seed, steps, warmup, cfg=None, kinds=("fp4", "bf16")):
     """One synthetic FLUX.1-dev DiT training step (19 double + 38 single
     blocks at 4096 image + 512 text tokens; forward, loss, backward, AdamW on
     the LoRA factors) with the W4A4G4 layers, and the same step with BF16
-    LoRA linears (the paper's comparison, Sec. 4 "Efficiency Results")."""
+    LoRA linears (the paper's comparison, Sec. 4 "Efficiency Results"); kind
+    "fp8": with 8-bit activations and gradients over the same weights."""
     from paper_2607_05711_amd import dit
     cfg = cfg or dit.FLUX_DEV
     out = {}
-    for kind in ("fp4", "bf16"):
+    for kind in kinds:
         torch.cuda.empty_cache()
         torch.cuda.reset_peak_memory_stats(dev)
         model = dit.DiT(cfg, kind, seed, dev)
@@ -743,7 +744,7 @@ def dit_step_timing(torch, dev, seed, steps, warmup, cfg=None):
         del model, trainer, batch
         print("dit %s: %.2f ms/step" % (kind, out[kind]["ms_per_step"]), file=sys.stderr, flush=True)
     return {"metric": "synthetic FLUX.1-dev DiT training step time, W4A4G4 vs BF16 LoRA", "unit": "ms",
-            "w4a4g4": out["fp4"], "bf16_lora": out["bf16"],
+            "w4a4g4": out["fp4"], "bf16_lora": out["bf16"], **({"w4a8g8": out["fp8"]} if "fp8" in out else {}),
             "speedup_vs_bf16_lora": round(out["bf16"]["ms_per_step"] / out["fp4"]["ms_per_step"], 3),
             "config": {"double_blocks": cfg.double_blocks, "single_blocks": cfg.single_blocks,
                        "img_tokens": cfg.img_tokens, "txt_tokens": cfg.txt_tokens, "hidden": cfg.hidden,
@@ -875,7 +876,8 @@ def run(args, sample_path):
         print(json.dumps(numerics_timing(torch, _lib, dev, args.seed, args.steps, args.warmup)), flush=True)
         return
     if args.dit:
-        print(json.dumps(dit_step_timing(torch, dev, args.seed, args.steps, args.warmup)), flush=True)
+        print(json.dumps(dit_step_timing(torch, dev, args.seed, args.steps, args.warmup, kinds=("fp4", "fp8", "bf16"))),
+              flush=True)
         return
     if args.stability:
         print(json.dumps(stability_probe(torch, _lib, dev, args.seed)), flush=True)

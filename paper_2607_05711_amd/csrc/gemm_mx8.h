@@ -16,10 +16,12 @@
 // and the loads of the stage NS further go out behind the second step's.
 // The weight's scales of the whole reduction stay in LDS.
 //
-// Bound by the matrix cores where there are many tiles: 18432 x 4096 -> 16384
-// takes 925 us (2.67 PFLOP/s), 4608 rows with GELU, z and R = 64 280 (2.24).  These
-// MFMAs from registers alone reach 3.8 to 4.0 PFLOP/s on random data, at which
-// the card lowers its clock (4.9 on constant data).  A 256 x 256 tile takes 1.28 us
+// Bound by the matrix cores where there are many tiles.  On three cards 18432 x
+// 4096 -> 16384 with SiLU takes 950 to 980 us (2.5 to 2.6 PFLOP/s), 4608 rows with
+// GELU, z and R = 64 285 to 305 (2.05 to 2.2; on one of them 281 over and over, 252
+// bare, 263 with R, 257 with GELU, 251 with z).  These MFMAs from registers alone
+// reach 3.8 to 4.0 PFLOP/s on random data, at which the card lowers its clock
+// (4.9 on constant data).  A 256 x 256 tile takes 1.28 us
 // a stage while all CUs run theirs and 0.98 alone: 3.35 PFLOP/s in the loop.  The
 // rest is a tile's start and end, some 10 us, of which little can hide: with
 // one wave a SIMD (128 x 128 outputs each, the fewest LDS reads per MFMA that
@@ -30,7 +32,8 @@
 // Where there are fewer tiles than CUs, latency counts: tiles of 64 x 128, at
 // most one a CU, are run by two groups of four waves that share the reduction
 // (333 x 3168 -> 2080 in fp32 16.5 us against 18.4; 128 x 4096 -> 4096 10.4
-// against 12.5).
+// against 12.5; in turn on one card).  The reduction is shared no further: few
+// outputs behind a long one wait for their stages (64 x 16384 -> 256 takes 28 us).
 //
 // An MFMA with an FP8 operand takes 64 cycles per wave and 32x32x64 products,
 // twice the FP4 time.  It adds its products in groups of eight consecutive
@@ -116,8 +119,9 @@ __global__ __launch_bounds__(256 * KG, TM > 128 ? 1 : 2) void k_gemm_mx8(
 
   // Each XCD takes a contiguous range of tiles, four tile-rows at a time, so
   // that its 32 CUs hold some 4 x 8 tiles whose operands meet in its L2: a byte
-  // of X serves 8 of them and a byte of W, half as many, 4.  (Eight tile-rows:
-  // 18432 x 4096 -> 16384 944 us against 925, 4608 rows 283 against 280.)
+  // of X serves 8 of them and a byte of W, half as many, 4.  (Eight tile-rows,
+  // in turn on one card: 18432 x 4096 -> 16384 944 us against 925, 4608 rows 283
+  // against 280.)
   const int T = tiles_m * tiles_n, per = (T + 7) >> 3;
   const int t = (blockIdx.x & 7) * per + (blockIdx.x >> 3);
   if (t >= T || (int)(blockIdx.x >> 3) >= per) return;   // the whole workgroup

@@ -18,12 +18,17 @@ bool gemm_mx8_supported(bool bwd, int M, int N, int K, int R) {
 // Which tile: the one of the least estimated time, in microseconds: rounds of
 // workgroups (one a CU on the wide tiles, two on the others, whose last round
 // may be of one) of a fixed part, the tile's start and end, and one per stage.
-// Measured and estimated, M x K -> N, 256x256 / 192x256 / 128x128 / 64x128:
-//   4608 x 4096 -> 16384   238 / 233 / 263 / 329    232 / 220 / 275 / 360
-//   4608 x 16384 -> 4096   306 / 247 / 260 / 300    323 / 252 / 274 / 298
-//   18432 x 4096 -> 16384  882 / 943 / 1074 / 1313  835 / 883 / 1100 / 1440
-//   2048 x 4096 -> 4096    44 / 36 / 33 / 42        46 / 37 / 31 / 40
-//   512 x 4096 -> 4096     40 / 32 / 18 / 13        46 / 37 / 17 / 11
+// Forward in bf16, the bare product over and over, measured and estimated, M x K ->
+// N, 256x256 / 192x256 / 128x128 / 64x128:
+//   4608 x 4096 -> 16384   256 / 243 / 272 / 329    232 / 221 / 275 / 360
+//   4608 x 16384 -> 4096   311 / 244 / 264 / 309    323 / 252 / 274 / 298
+//   18432 x 4096 -> 16384  906 / 954 / 1077 / 1351  835 / 882 / 1100 / 1440
+//   2048 x 4096 -> 4096    47 / 38 / 33 / 41        46 / 37 / 31 / 40
+//   512 x 4096 -> 4096     41 / 32 / 19 / 13        46 / 37 / 17 / 11
+// The input gradient is within a tenth of these.  fp32 results have twice the
+// matrix time and the same order, so the estimate serves them too: 446 / 418 / 445 /
+// 509, 608 / 459 / 448 / 469 (the choice of 192 costs 2 %), 1652 / 1671 / 1822 / 2033,
+// 88 / 70 / 56 / 63, 80 / 63 / 33 / 20.  The low-rank term's stages weigh the same on all.
 int gemm_mx8_tile(bool bwd, int M, int N, int K) {
   const long NO = bwd ? K : N, nst = ((bwd ? N : K) + 127) / 128;
   const struct { int tm, tn, cap; double fix, stage, fix1, stage1; size_t slot; } t[] = {

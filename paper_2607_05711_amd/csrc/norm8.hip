@@ -111,10 +111,11 @@ __global__ __launch_bounds__(256) void k_rmsnorm_q8(const uint16_t* x, const uin
 hipError_t launch_rmsnorm_q8(const uint16_t* x, const uint16_t* res, const uint16_t* w, float eps, int rows, int K,
                              uint16_t* h, uint16_t* y, uint8_t* codes, uint8_t* scales, float* rstd, hipStream_t st) {
   // A workgroup a row where rows are long or too few to fill the chip with one
-  // wave each: 4608 x 4096 with every output 26.0 us against 34.8 on one wave a
-  // row (whose 244 registers leave two waves a SIMD); 4608 x 1024 9.1 against 8.3,
-  // 18432 x 1024 without y 25.0 against 21.1, where a workgroup's four waves
-  // would be half idle.
+  // wave each.  With residual, on inputs that no cache holds: 4608 x 4096 with
+  // every output 37.3 us against 49.7 on one wave a row (whose 244 registers leave
+  // two waves a SIMD), 18432 x 2048 65.6 against 72.5, 4608 x 2048 20.3 against
+  // 19.6; 4608 x 1024 12.8 against 11.3 and 18432 x 1024 without y 33.6 against 29.1,
+  // where a workgroup's four waves would be half idle (2500 x 1024: 8.6 against 7.9).
   const bool wide = K > 2048 || rows < 4096;
   const int nc = (K + (wide ? 2047 : 511)) / (wide ? 2048 : 512);
   const int nwg = (wide ? rows : (rows + 3) / 4);
@@ -284,8 +285,9 @@ __global__ __launch_bounds__(256) void k_rmsnorm_dw(const float* __restrict__ pa
 namespace {
 struct BwdPlan { bool wide; int nc, groups; };
 // As in the forward; 512 workgroups (two a CU) or fewer, since each leaves a row
-// of partial sums: 4608 x 4096 28.8 us with 512, 31.1 with 768, 32.2 with 1024; 38.4
-// on one wave a row.
+// of partial sums.  Both launches, with dh, on inputs that no cache holds: 4608 x
+// 4096 34.4 us with 512, 37.1 with 768, 39.8 with 1024; 44.1 on one wave a row, which
+// 18432 x 1024 takes in 32.4 against 39.6.
 BwdPlan bwd_plan(int rows, int K) {
   const bool wide = K > 2048 || rows < 2048;
   const int units = wide ? rows : (rows + 3) / 4;

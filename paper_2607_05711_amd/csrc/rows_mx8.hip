@@ -146,8 +146,8 @@ __global__ __launch_bounds__(64 * RW) void k_rows_mx8(const uint8_t* __restrict_
 }
 
 // Against the tile kernel (64 x 128 tiles), us a call, M x K -> N: 16 x 4096 -> 16384
-// 10.6 against 12.4, 16 x 16384 -> 4096 14 against 29, 32 x 4096 -> 4096 9.4 against
-// 11.3; but every workgroup reads X, in rows of 128 bytes a step: 64 x 4096 -> 4096
+// 10.9 against 12.7, 16 x 16384 -> 4096 14 against 29, 32 x 4096 -> 4096 9.4 against
+// 11.1; but every workgroup reads X, in rows of 128 bytes a step: 64 x 4096 -> 4096
 // took 16 against 11.
 bool rows_mx8_better(int M, int N) { return M <= 16 || (M <= kRowsMx8Max && N <= 8192); }
 
