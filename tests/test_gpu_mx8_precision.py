@@ -93,7 +93,8 @@ def test_what_product_groups_drop(tile, back, outliers, on_tile):
     off = (y - left).abs()
     tol = (total + fp32) * (1 + 2.0 ** -8) + left.abs() * 2.0 ** -8
     assert bool((off <= tol).all()), float((off / tol).max())
-    assert float(off.norm()) <= float(rms.norm() + fp32.norm() + left.norm() * 2.0 ** -8)
+    # (partial sums of random terms are on average no larger than the whole; twice their roundings' share)
+    assert float(off.norm()) <= float(rms.norm() + (1024 / 8 + 2) ** 0.5 * 2.0 ** -23 * want.norm() + left.norm() * 2.0 ** -8)
     # and fp32 results, whose groups are exact
     exact = f(xq, xs, wq, ws, out_dtype=F32).double()
     assert bool(((exact - want).abs() <= 2 * fp32 + want.abs() * 2.0 ** -24).all())
