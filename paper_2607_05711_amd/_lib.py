@@ -164,11 +164,17 @@ def _need(t, name, dtype, device=None, ndim=None):
 
 
 def _workspace(nbytes, dev, workspace):
-    """The caller's workspace (checked for size) or a new one of nbytes."""
+    """The caller's workspace (checked for size, place and layout) or a new one of nbytes; dev: a device or its number."""
     if nbytes == 0:
         return workspace
     if workspace is None:
         return torch.empty(((nbytes + 15) // 16) * 16, dtype=torch.uint8, device=dev)
+    if not isinstance(workspace, torch.Tensor):
+        raise TypeError("workspace must be a torch.Tensor")
+    if not workspace.is_cuda or workspace.get_device() != (dev if isinstance(dev, int) else dev.index):
+        raise ValueError("workspace is on %s, expected GPU %s" % (workspace.device, dev))
+    if not workspace.is_contiguous():
+        raise ValueError("workspace must be contiguous")
     if workspace.numel() * workspace.element_size() < nbytes:
         raise ValueError("workspace of %d bytes, %d required" % (workspace.numel() * workspace.element_size(), nbytes))
     return workspace

@@ -192,3 +192,29 @@ def test_kernel_of_a_product(back, M, K, N, want):
     f = _lib.load().ftx_linear8_tile
     f.argtypes, f.restype = [ctypes.c_int] + [ctypes.c_int64] * 3, ctypes.c_int
     assert f(int(back), M, N, K) == want
+
+
+def test_workspaces_that_a_kernel_cannot_write():
+    """A workspace in host memory, or one whose elements share their storage, is refused whatever its size."""
+    dev = torch.device("cuda", 0)
+    for d in (dev, 0):
+        for ws in (torch.empty(1 << 12, dtype=torch.uint8), torch.empty(1 << 12, dtype=torch.uint8, device="meta"), b"0" * 4096):
+            with pytest.raises((ValueError, TypeError)):
+                _lib._workspace(64, d, ws)
+            with pytest.raises((ValueError, TypeError)):
+                _lib._space(64, d, ws)
+    assert _lib._space(0, 0, None) == (None, None, 0)
+
+
+@pytest.mark.gpu
+def test_workspaces_on_the_gpu():
+    g = ref.gen(1)
+    dy, w, r = ref.normal(g, 40, 64), ref.normal(g, 64), torch.ones(40, device="cuda:0")
+    n = _lib.ft_rmsnorm_bwd_workspace_size(40, 64)
+    whole = torch.empty(2 * n, dtype=torch.uint8, device="cuda:0")
+    for ws in (whole[:1].expand(2 * n), whole[::2], torch.empty(n, dtype=torch.uint8), whole[:n - 16]):
+        with pytest.raises(ValueError):
+            _lib.ft_rmsnorm_bwd(dy, dy, w, r, workspace=ws)
+    want = _lib.ft_rmsnorm_bwd(dy, dy, w, r)[1]
+    for ws in (whole, whole[:n], whole[16:].view(torch.float32)):
+        assert torch.equal(_lib.ft_rmsnorm_bwd(dy, dy, w, r, workspace=ws)[1], want)
